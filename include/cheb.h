@@ -287,6 +287,73 @@ CHEB_API int cheb_cache_destroy(cheb_cache *c);
  * are. */
 CHEB_API int cheb_cache_reset(cheb_cache *c);
 
+/* ---- 8-bit entries. -------------------------------------------------------
+ *
+ * A history whose entries hold 8 bits an element (plus a scale byte for 32):
+ * about half a bf16 history's memory and prediction time.  cheb_cache_push
+ * quantises the step's tensors, which stay of the cache's storage type, as it
+ * stores them; predictions, residual updates and cheb_cache_read decode the
+ * entries and give the storage type (or the fp32 residual).  The calls are
+ * those of any cache; exceptions are named below.
+ *
+ * The formats are the OCP microscaling ones with 32 consecutive elements of a
+ * cached tensor to a group and one power-of-two scale 2^e (E8M0) for it.  With
+ * a = max |x| of the group, e is the least integer with a <= L 2^e, kept within
+ * [-120, 127]:
+ *   CHEB_QUANT_MXINT8  L = 127/64: code = x 2^(6-e), rounded to nearest even
+ *                      (and to +-127 where a exceeds 127 2^121), standing for
+ *                      code 2^(e-6).  Off by at most 2^(e-7), half a step: under
+ *                      a / 127.  The closer one where a group's values are
+ *                      alike, which an extrapolation's large weights ask for.
+ *   CHEB_QUANT_MXFP8   L = 448: code = x 2^-e rounded to nearest even as e4m3,
+ *                      standing for its value times 2^e.  Off by at most 2^-4 of
+ *                      the value, or 2^(e-10) below 2^(e-6): keeps small values
+ *                      beside a large one.
+ * A group with a NaN or an infinity reads back as NaN, all of it.  A value
+ * whose code stands for more than the storage type holds reads back as infinity
+ * (fp16: beyond 65023 for MXINT8, 63487 for MXFP8).  Predictions sum in fp32 for
+ * bf16 and fp16 caches and in fp64 for fp32 ones; residual updates sum the
+ * entries of one tensor in fp32 and tensors in fp64. */
+enum { CHEB_QUANT_NONE = 0, CHEB_QUANT_MXINT8 = 1, CHEB_QUANT_MXFP8 = 2 };
+
+/* The layout of a history of 8-bit entries: as cheb_cache_layout, but cached
+ * tensors start on multiples of 4096 elements, in outputs too, and the padding
+ * elements of entries, and so of predictions, are zero unless the tensor's last
+ * group is NaN.  How an entry lies in the arena is the library's own.
+ *   quant   CHEB_QUANT_MXINT8 or CHEB_QUANT_MXFP8.
+ *   layout  CHEB_LAYOUT_SLOTS, or CHEB_LAYOUT_INTERLEAVED for entries cut into
+ *           chunks taken in turn, which predictions read faster.
+ *   seg_offset [n_segs], slot_numel, arena_bytes: out, each may be NULL.
+ * Other arguments as cheb_cache_layout.  Errors: CHEB_E_INVAL, CHEB_E_DTYPE. */
+CHEB_API int cheb_cache_layout_quant(int32_t n_slots, int32_t dtype, int32_t quant,
+                                     const int64_t *seg_numel, int32_t n_segs, int32_t layout,
+                                     int64_t *seg_offset, int64_t *slot_numel,
+                                     size_t *arena_bytes);
+
+/* cheb_cache_create_ex for 8-bit entries; arena_bytes at least those of
+ * cheb_cache_layout_quant.  Every cache call takes the handle but
+ * cheb_cache_begin_push (a module cannot write codes), cheb_cache_entry and
+ * cheb_cache_geometry (read entries with cheb_cache_read), which fail with
+ * CHEB_E_INVAL.  In cheb_residual_apply, offsets and sizes of added segments
+ * and of the residual are multiples of 8 elements for every storage type, and
+ * weights are of fp32's range.  Errors: as cheb_cache_create_ex. */
+CHEB_API int cheb_cache_create_quant(cheb_cache **out, int32_t n_slots, int32_t dtype,
+                                     int32_t quant, const int64_t *seg_numel, int32_t n_segs,
+                                     int32_t layout, void *arena, size_t arena_bytes);
+
+/* Format of the cache's entries: CHEB_QUANT_NONE for one that stores its
+ * elements as they are.  Errors: CHEB_E_INVAL. */
+CHEB_API int cheb_cache_quant(const cheb_cache *c, int32_t *quant);
+
+/* The features f_{s_j} of held entry j = `idx`, counted from the oldest (0), as
+ * one contiguous entry of the storage type: of any cache, whatever its layout,
+ * and of 8-bit entries the values that their codes stand for.
+ *   out  device, 16-byte aligned, cheb_cache_slot_numel elements, not
+ *        overlapping the arena.
+ * Errors: CHEB_E_INVAL (also idx outside 0 .. count-1), CHEB_E_NOTREADY (a
+ * fused push is open), CHEB_E_ALIGN, CHEB_E_HIP. */
+CHEB_API int cheb_cache_read(cheb_cache *c, int32_t idx, void *out, void *stream);
+
 /* Stores the full step at abscissa t: copies segment s from seg_src[s]
  * (device, 16-byte aligned, seg_numel[s] elements) into the slot of the
  * oldest entry (or the next free one), zero-fills the padding after each

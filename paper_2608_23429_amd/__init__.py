@@ -14,7 +14,9 @@ import torch
 
 from ._binding import (  # noqa: F401  (re-exported C entry points)
     CHEB_LAYOUT_INTERLEAVED, CHEB_LAYOUT_SLOTS, cheb_cache_arena_bytes_ex, cheb_cache_create_ex,
-    cheb_cache_geometry, DEFAULT_LAUNCH_CONFIG,
+    cheb_cache_geometry, DEFAULT_LAUNCH_CONFIG, CHEB_QUANT_MXFP8, CHEB_QUANT_MXINT8,
+    CHEB_QUANT_NONE, cheb_cache_create_quant, cheb_cache_layout_quant, cheb_cache_quant,
+    cheb_cache_read,
     CHEB_BF16, CHEB_F16, CHEB_F32, CHEB_MAX_NODES, CHEB_MAX_OUTPUTS, CHEB_MAX_SLOTS, CHEB_RHO_ALTERNATING,
     CHEB_RHO_GENERAL, CHEB_SHORT_FULL, CHEB_TAYLOR, CHEB_SHORT_LOWER, ChebError, cheb_chebyshev_nodes,
     cheb_precompute_weights_variant,
@@ -252,6 +254,7 @@ class ResidualHistory:
         self.cache.close()
 
 
+_QUANTS = {None: CHEB_QUANT_NONE, "mxint8": CHEB_QUANT_MXINT8, "mxfp8": CHEB_QUANT_MXFP8}
 _LAYOUTS = {"slots": CHEB_LAYOUT_SLOTS, "interleaved": CHEB_LAYOUT_INTERLEAVED}
 
 
@@ -263,11 +266,15 @@ class ChebCache:
     layout; ``segment_views`` cuts a flat buffer into per-segment views.
     ``layout`` is "slots" (contiguous entries; fused push possible) or
     "interleaved" (entries cut into 32 KiB chunks taken in turn; filled by
-    ``push``).
+    ``push``).  ``quant`` is None (entries of ``dtype``) or a format of 8-bit
+    entries, "mxint8" or "mxfp8": ``push`` then quantises tensors of ``dtype``
+    in groups of 32 elements, and predictions, ``read`` and the residual update
+    decode them; tensors start on multiples of 4096 elements.
     """
 
     def __init__(self, n_slots: int, dtype: torch.dtype, seg_numel: Sequence[int],
-                 device=None, arena: Optional[torch.Tensor] = None, layout: str = "slots"):
+                 device=None, arena: Optional[torch.Tensor] = None, layout: str = "slots",
+                 quant: Optional[str] = None):
         self.n_slots = int(n_slots)
         self.dtype = dtype
         self.cdtype = cheb_dtype(dtype)
@@ -275,18 +282,31 @@ class ChebCache:
         if layout not in _LAYOUTS:
             raise ChebError(_binding.CHEB_E_INVAL, f"unknown layout {layout!r}")
         self.layout = layout
-        lay = cheb_cache_layout(self.n_slots, self.cdtype, self.seg_numel)
+        if quant not in _QUANTS:
+            raise ChebError(_binding.CHEB_E_INVAL, f"unknown 8-bit format {quant!r}")
+        self.quant = quant
+        if quant is None:
+            lay = cheb_cache_layout(self.n_slots, self.cdtype, self.seg_numel)
+            self.slot_stride_bytes = int(lay["slot_stride_bytes"])
+            self.arena_bytes = cheb_cache_arena_bytes_ex(self.n_slots, self.cdtype,
+                                                         self.seg_numel, _LAYOUTS[layout])
+        else:
+            lay = cheb_cache_layout_quant(self.n_slots, self.cdtype, _QUANTS[quant],
+                                          self.seg_numel, _LAYOUTS[layout])
+            self.arena_bytes = int(lay["arena_bytes"])
         self.seg_offset = [int(o) for o in lay["seg_offset"]]
         self.slot_numel = int(lay["slot_numel"])
-        self.slot_stride_bytes = int(lay["slot_stride_bytes"])
-        self.arena_bytes = cheb_cache_arena_bytes_ex(self.n_slots, self.cdtype, self.seg_numel,
-                                                     _LAYOUTS[layout])
         if arena is None:
             device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
             arena = torch.empty(self.arena_bytes, dtype=torch.uint8, device=device)
         _check_device_tensor(arena, "arena")
         self.arena = arena
         self.device = arena.device
+        if quant is not None:
+            self._h = cheb_cache_create_quant(self.n_slots, self.cdtype, _QUANTS[quant],
+                                              self.seg_numel, _LAYOUTS[layout], arena.data_ptr(),
+                                              arena.numel() * arena.element_size())
+            return
         self._h = cheb_cache_create_ex(self.n_slots, self.cdtype, self.seg_numel, _LAYOUTS[layout],
                                        arena.data_ptr(), arena.numel() * arena.element_size())
         _, self.chunk_elems, self.entry_stride_elems = cheb_cache_geometry(self._h)
@@ -326,7 +346,10 @@ class ChebCache:
     def entry(self, idx: int) -> torch.Tensor:
         """The held entry of age index idx (0 = oldest) as a flat tensor: a
         view of its slot in the slot layout, a gathered copy of its chunks
-        in the interleaved layout."""
+        in the interleaved layout, the values of its codes where entries are
+        held in 8 bits."""
+        if self.quant is not None:
+            return self.read(idx)
         addr = cheb_cache_entry(self._h, idx)
         if self.layout == "slots":
             return self._slot_tensor(addr)
@@ -340,6 +363,15 @@ class ChebCache:
         chunks = torch.as_strided(whole, (n_chunks, chunk), (stride, 1),
                                   storage_offset=whole.storage_offset() + start)
         return chunks.reshape(-1)[:self.slot_numel].clone()
+
+    def read(self, idx: int, out: Optional[torch.Tensor] = None,
+             stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """The held entry of age index idx (0 = oldest) as a flat tensor of its
+        own, whatever the layout; of 8-bit entries the values of the codes."""
+        out = self.new_output() if out is None else out
+        self._check_out(out)
+        cheb_cache_read(self._h, idx, out.data_ptr(), _stream_handle(stream))
+        return out
 
     # -- the online stage ------------------------------------------------------
     def push(self, t: float, segments: Sequence[torch.Tensor],

@@ -37,6 +37,10 @@ CHEB_TAYLOR = 2
 CHEB_LAYOUT_SLOTS = 0
 CHEB_LAYOUT_INTERLEAVED = 1
 
+CHEB_QUANT_NONE = 0
+CHEB_QUANT_MXINT8 = 1
+CHEB_QUANT_MXFP8 = 2
+
 CHEB_BF16 = 0
 CHEB_F32 = 1
 CHEB_F16 = 2
@@ -101,6 +105,13 @@ SIGNATURES = {
                           _i64p, _szp, _szp],
     "cheb_cache_create": [ctypes.POINTER(_vp), ctypes.c_int32, ctypes.c_int32, _i64p,
                           ctypes.c_int32, _vp, ctypes.c_size_t],
+    "cheb_cache_layout_quant": [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _i64p,
+                                ctypes.c_int32, ctypes.c_int32, _i64p, _i64p, _szp],
+    "cheb_cache_create_quant": [ctypes.POINTER(_vp), ctypes.c_int32, ctypes.c_int32,
+                                ctypes.c_int32, _i64p, ctypes.c_int32, ctypes.c_int32, _vp,
+                                ctypes.c_size_t],
+    "cheb_cache_quant": [_vp, _i32p],
+    "cheb_cache_read": [_vp, ctypes.c_int32, _vp, _vp],
     "cheb_cache_destroy": [_vp],
     "cheb_cache_reset": [_vp],
     "cheb_cache_push": [_vp, ctypes.c_double, _vpp, _vp],
@@ -312,6 +323,37 @@ def cheb_cache_create(n_slots, dtype, seg_numel, arena_ptr, arena_bytes):
                                  seg.ctypes.data_as(_i64p), seg.size,
                                  ctypes.c_void_p(int(arena_ptr)), int(arena_bytes)))
     return h
+
+
+def cheb_cache_layout_quant(n_slots, dtype, quant, seg_numel, layout):
+    seg = np.ascontiguousarray(seg_numel, dtype=np.int64).reshape(-1)
+    off = np.empty_like(seg)
+    slot_numel = ctypes.c_int64()
+    arena = ctypes.c_size_t()
+    _check(LIB.cheb_cache_layout_quant(int(n_slots), int(dtype), int(quant),
+                                       seg.ctypes.data_as(_i64p), seg.size, int(layout),
+                                       off.ctypes.data_as(_i64p), ctypes.byref(slot_numel),
+                                       ctypes.byref(arena)))
+    return {"seg_offset": off, "slot_numel": slot_numel.value, "arena_bytes": arena.value}
+
+
+def cheb_cache_create_quant(n_slots, dtype, quant, seg_numel, layout, arena_ptr, arena_bytes):
+    seg = np.ascontiguousarray(seg_numel, dtype=np.int64).reshape(-1)
+    h = ctypes.c_void_p()
+    _check(LIB.cheb_cache_create_quant(ctypes.byref(h), int(n_slots), int(dtype), int(quant),
+                                       seg.ctypes.data_as(_i64p), seg.size, int(layout),
+                                       ctypes.c_void_p(int(arena_ptr)), int(arena_bytes)))
+    return h
+
+
+def cheb_cache_quant(handle) -> int:
+    q = ctypes.c_int32()
+    _check(LIB.cheb_cache_quant(handle, ctypes.byref(q)))
+    return q.value
+
+
+def cheb_cache_read(handle, idx, out_ptr, stream=0):
+    _check(LIB.cheb_cache_read(handle, int(idx), int(out_ptr), int(stream)))
 
 
 def cheb_cache_destroy(handle):

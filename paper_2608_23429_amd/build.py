@@ -9,6 +9,7 @@ import os
 import shutil
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -20,8 +21,8 @@ BUILD_DIR = os.path.join(ROOT, "_build", "cheb")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 ARCH = "gfx950"
 
-HOST_SOURCES = ["api.cpp", "cache.cpp", "table.cpp", "residual.cpp"]
-DEVICE_SOURCES = ["kernels.hip"]
+HOST_SOURCES = ["api.cpp", "cache.cpp", "table.cpp", "residual.cpp", "coded.cpp"]
+DEVICE_SOURCES = ["kernels.hip", "coded.hip", "predict_coded.hip"]
 
 DEVICE_FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",
@@ -53,15 +54,14 @@ def build(verbose: bool = False) -> str:
     if not os.path.exists(cxx):
         cxx = shutil.which("g++") or "g++"
     incs = ["-I", INCLUDE, "-I", CSRC, "-I", os.path.join(ROCM, "include")]
-    objs = []
-    for src in HOST_SOURCES:
-        obj = os.path.join(BUILD_DIR, src + ".o")
-        _run([cxx, *HOST_FLAGS, *incs, "-c", os.path.join(CSRC, src), "-o", obj], verbose)
-        objs.append(obj)
-    for src in DEVICE_SOURCES:
-        obj = os.path.join(BUILD_DIR, src + ".o")
-        _run([hipcc, *DEVICE_FLAGS, *incs, "-c", os.path.join(CSRC, src), "-o", obj], verbose)
-        objs.append(obj)
+    cmds, objs = [], []
+    for compiler, sources in ([hipcc, *DEVICE_FLAGS], DEVICE_SOURCES), ([cxx, *HOST_FLAGS],
+                                                                        HOST_SOURCES):
+        for src in sources:
+            objs.append(os.path.join(BUILD_DIR, src + ".o"))
+            cmds.append([*compiler, *incs, "-c", os.path.join(CSRC, src), "-o", objs[-1]])
+    with ThreadPoolExecutor(max_workers=4) as pool:   # the kernel sources take a minute or two each
+        list(pool.map(lambda cmd: _run(cmd, verbose), cmds))
     tmp = LIB + ".tmp"
     _run([hipcc, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs,
           "-Wl,--no-undefined", "-Wl,-soname,libcheb.so"], verbose)

@@ -25,6 +25,11 @@ int g_lds[kMaxDevices] = {0};
 std::mutex g_cus_mutex;
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+bool overlap(const void *a, const void *b, uintptr_t bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + bytes && y < x + bytes;
+}
 }  // namespace
 
 int fail(int code, const char *fmt, ...) {
@@ -357,16 +362,13 @@ int cheb_combine(const void *const *src, int32_t n_src, const double *w, void *o
 
 namespace cheb {
 
-int combine_checked(const void *const *src, int32_t n_src, const double *w, int32_t n_out,
-                    void *const *out, int64_t numel, int32_t dtype, int64_t super_vecs,
-                    void *stream) {
-  const bool contiguous = super_vecs == kChunkVecs;
+int check_weights(const double *w, int32_t n_src, int32_t n_out, int64_t numel, int32_t dtype) {
   if (!valid_dtype(dtype)) return fail(CHEB_E_DTYPE, "unknown dtype %d", dtype);
   if (n_src < 1 || n_src > CHEB_MAX_SLOTS)
     return fail(CHEB_E_INVAL, "n_src %d outside 1..%d", n_src, CHEB_MAX_SLOTS);
   if (n_out < 1 || n_out > CHEB_MAX_OUTPUTS)
     return fail(CHEB_E_INVAL, "n_out %d outside 1..%d", n_out, CHEB_MAX_OUTPUTS);
-  if (!src || !w || !out) return fail(CHEB_E_INVAL, "src, w or out is NULL");
+  if (!w) return fail(CHEB_E_INVAL, "src, w or out is NULL");
   if (numel < 0) return fail(CHEB_E_INVAL, "numel is negative");
   if (numel / elems_per_vec(dtype) >= kMaxVecs)
     return fail(CHEB_E_INVAL, "numel %lld too large for one launch", (long long)numel);
@@ -376,29 +378,45 @@ int combine_checked(const void *const *src, int32_t n_src, const double *w, int3
     if (dtype != CHEB_F32 && fabs(w[m]) > double(FLT_MAX))
       return fail(CHEB_E_NONFINITE, "weight %d (%.17g) overflows fp32", m, w[m]);
   }
+  return CHEB_OK;
+}
+
+int check_outputs(int32_t n_out, void *const *out, int64_t numel, int32_t dtype) {
+  const uintptr_t bytes = uintptr_t(numel) * uintptr_t(elem_bytes(dtype));
+  for (int m = 0; m < n_out; ++m) {
+    if (!out[m]) return fail(CHEB_E_INVAL, "out[%d] is NULL", m);
+    if (!aligned16(out[m])) return fail(CHEB_E_ALIGN, "out[%d] is not 16-byte aligned", m);
+    for (int j = 0; j < m; ++j)
+      if (overlap(out[m], out[j], bytes))
+        return fail(CHEB_E_INVAL, "out[%d] overlaps out[%d]", m, j);
+  }
+  return CHEB_OK;
+}
+
+int combine_checked(const void *const *src, int32_t n_src, const double *w, int32_t n_out,
+                    void *const *out, int64_t numel, int32_t dtype, int64_t super_vecs,
+                    void *stream) {
+  const bool contiguous = super_vecs == kChunkVecs;
+  if (!src || !out) w = nullptr;
+  int rc = check_weights(w, n_src, n_out, numel, dtype);
+  if (rc != CHEB_OK) return rc;
   if (!contiguous && numel % elems_per_vec(dtype) != 0)
     return fail(CHEB_E_INVAL, "interleaved sources need whole 16-byte vectors");
   if (numel == 0) return ok();
-  const uintptr_t bytes = uintptr_t(numel) * elem_bytes(dtype);
-  auto overlap = [bytes](const void *a, const void *b) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x < y + bytes && y < x + bytes;
-  };
   for (int k = 0; k < n_src; ++k) {
     if (!src[k]) return fail(CHEB_E_INVAL, "src[%d] is NULL", k);
     if (!aligned16(src[k])) return fail(CHEB_E_ALIGN, "src[%d] is not 16-byte aligned", k);
   }
-  for (int m = 0; m < n_out; ++m) {
-    if (!out[m]) return fail(CHEB_E_INVAL, "out[%d] is NULL", m);
-    if (!aligned16(out[m])) return fail(CHEB_E_ALIGN, "out[%d] is not 16-byte aligned", m);
-    // Interleaved sources spread over their arena; the cache checks the
-    // outputs against the whole arena instead.
-    if (contiguous)
+  rc = check_outputs(n_out, out, numel, dtype);
+  if (rc != CHEB_OK) return rc;
+  // Interleaved sources spread over their arena; the cache checks the
+  // outputs against the whole arena instead.
+  const uintptr_t bytes = uintptr_t(numel) * uintptr_t(elem_bytes(dtype));
+  if (contiguous)
+    for (int m = 0; m < n_out; ++m)
       for (int k = 0; k < n_src; ++k)
-        if (overlap(out[m], src[k])) return fail(CHEB_E_INVAL, "out[%d] overlaps src[%d]", m, k);
-    for (int j = 0; j < m; ++j)
-      if (overlap(out[m], out[j])) return fail(CHEB_E_INVAL, "out[%d] overlaps out[%d]", m, j);
-  }
+        if (overlap(out[m], src[k], bytes))
+          return fail(CHEB_E_INVAL, "out[%d] overlaps src[%d]", m, k);
   return launch_combine(dtype, src, n_src, w, n_out, out, numel, super_vecs,
                         static_cast<hipStream_t>(stream));
 }

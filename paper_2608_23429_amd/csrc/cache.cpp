@@ -9,38 +9,9 @@
 #include <new>
 #include <vector>
 
-#include "internal.h"
+#include "cache.h"
 
 using namespace cheb;
-
-struct cheb_cache {
-  int32_t n_slots = 0;
-  int32_t dtype = CHEB_BF16;
-  std::vector<int64_t> seg_numel;
-  std::vector<int64_t> seg_offset;
-  int64_t slot_numel = 0;
-  size_t slot_stride = 0;
-  char *arena = nullptr;
-  size_t arena_bytes = 0;
-  int32_t layout = CHEB_LAYOUT_SLOTS;
-  char *region = nullptr;          // interleaved: first lane, on a kLaneAlign boundary
-  int64_t super_vecs = kChunkVecs; // chunk stride of an entry (vectors)
-  // Ring state: `head` is the slot the next entry goes to; the `count` held
-  // entries, oldest first, are in slots head - count, ..., head - 1 (mod n).
-  double slot_t[CHEB_MAX_SLOTS] = {0};
-  int32_t head = 0;
-  int32_t count = 0;
-  bool push_open = false;
-
-  int32_t slot_of_age(int32_t age) const {
-    return ((head - count + age) % n_slots + n_slots) % n_slots;
-  }
-  // Base of the entry stored in `slot` (its first vector).
-  char *slot_ptr(int32_t slot) const {
-    return layout == CHEB_LAYOUT_SLOTS ? arena + size_t(slot) * slot_stride
-                                       : region + size_t(slot) * kChunkBytes;
-  }
-};
 
 namespace {
 
@@ -135,6 +106,14 @@ int extrapolate_newest(cheb_cache *c, int32_t used, const double *w, int32_t n_o
         return fail(CHEB_E_INVAL, "out[%d] overlaps the cache arena", m);
     }
   }
+  if (c->coded) {
+    int rc = check_weights(w, used, n_out, c->slot_numel, c->dtype);
+    if (rc != CHEB_OK) return rc;
+    if (c->slot_numel == 0) return ok();
+    rc = check_outputs(n_out, out, c->slot_numel, c->dtype);
+    if (rc != CHEB_OK) return rc;
+    return c->coded->predict(c, 0, used, w, n_out, out, static_cast<hipStream_t>(stream));
+  }
   return combine_checked(src, used, w, n_out, out, c->slot_numel, c->dtype, c->super_vecs,
                          stream);
 }
@@ -151,6 +130,7 @@ int cache_view(const cheb_cache *c, CacheView *v) {
   v->slot_numel = c->slot_numel;
   v->layout = c->layout;
   v->super_vecs = c->super_vecs;
+  v->coded = c->coded;
   v->arena = c->arena;
   v->arena_bytes = c->arena_bytes;
   return CHEB_OK;
@@ -316,6 +296,7 @@ int cheb_cache_create(cheb_cache **out, int32_t n_slots, int32_t dtype, const in
 int cheb_cache_geometry(const cheb_cache *c, int32_t *layout_kind, int64_t *chunk_elems,
                         int64_t *entry_stride_elems) {
   if (!c) return fail(CHEB_E_INVAL, "cache is NULL");
+  if (c->coded) return fail(CHEB_E_INVAL, "8-bit entries are read with cheb_cache_read");
   const int64_t vec = elems_per_vec(c->dtype);
   if (layout_kind) *layout_kind = c->layout;
   if (chunk_elems) *chunk_elems = kChunkVecs * vec;
@@ -357,8 +338,11 @@ int cheb_cache_push(cheb_cache *c, double t, const void *const *seg_src, void *s
   // first launch, so a launch that fails after an earlier one has written
   // part of the slot cannot leave a half-overwritten entry in the history.
   const int32_t slot = claim_slot(c);
-  rc = launch_gather(c->dtype, c->slot_ptr(slot), segs.data(), int(n_segs), c->super_vecs,
-                     static_cast<hipStream_t>(stream));
+  if (c->coded)
+    rc = c->coded->push(c, slot, seg_src, static_cast<hipStream_t>(stream));
+  else
+    rc = launch_gather(c->dtype, c->slot_ptr(slot), segs.data(), int(n_segs), c->super_vecs,
+                       static_cast<hipStream_t>(stream));
   if (rc != CHEB_OK) return rc;
   record(c, t);
   return ok();
@@ -366,6 +350,7 @@ int cheb_cache_push(cheb_cache *c, double t, const void *const *seg_src, void *s
 
 int cheb_cache_begin_push(cheb_cache *c, void **slot_base) {
   if (!c || !slot_base) return fail(CHEB_E_INVAL, "cache or slot_base is NULL");
+  if (c->coded) return fail(CHEB_E_INVAL, "8-bit entries are filled by cheb_cache_push");
   if (c->layout != CHEB_LAYOUT_SLOTS)
     return fail(CHEB_E_INVAL, "a fused push needs contiguous slots (CHEB_LAYOUT_SLOTS)");
   if (c->push_open) return fail(CHEB_E_NOTREADY, "a fused push is already open");
@@ -404,6 +389,7 @@ int cheb_cache_history(const cheb_cache *c, double *t_out, int32_t *count) {
 
 int cheb_cache_entry(const cheb_cache *c, int32_t idx, void **slot_base) {
   if (!c || !slot_base) return fail(CHEB_E_INVAL, "cache or slot_base is NULL");
+  if (c->coded) return fail(CHEB_E_INVAL, "8-bit entries are read with cheb_cache_read");
   if (idx < 0 || idx >= c->count)
     return fail(CHEB_E_INVAL, "entry %d outside 0..%d", idx, c->count - 1);
   *slot_base = c->slot_ptr(c->slot_of_age(idx));

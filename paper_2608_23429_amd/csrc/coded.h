@@ -1,0 +1,217 @@
+// Device code of the 8-bit formats: codes and scales from the values of a
+// group, and values from codes.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <stdint.h>
+#include <string.h>
+
+namespace cheb {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+// A group's scale byte (2^(scale - 127), 255: NaN) and the factor that takes
+// values to codes (0 for a group that is not finite: its codes are 0, and 0
+// times the scale's infinity, 255 << 23, is NaN).
+struct Group {
+  uint32_t scale;
+  float factor;
+  bool top;  // its largest value may round past the largest code
+};
+
+// The largest of four neighbouring lanes' values, by two exchanges.
+__device__ __forceinline__ uint32_t quad_max(uint32_t m) {
+  m = max(m, uint32_t(__builtin_amdgcn_mov_dpp(int(m), 0xB1, 0xF, 0xF, true)));  // 1 0 3 2
+  return max(m, uint32_t(__builtin_amdgcn_mov_dpp(int(m), 0x4E, 0xF, 0xF, true)));  // 2 3 0 1
+}
+
+// From the bits of the group's largest magnitude a (fp32): the exponent e, the
+// least with a <= L 2^e, is a's own less L's, one more where a's fraction
+// exceeds L's.
+template <class Fmt>
+__device__ __forceinline__ Group group_of(uint32_t a) {
+  const int e = int((a + (0x7fffffu - Fmt::kLimitFraction)) >> 23) - 127 - Fmt::kLimitExponent;
+  const int kept = min(max(e, -120), 127);
+  Group g;
+  g.top = e > 127;
+  g.scale = uint32_t(kept + 127);
+  g.factor = __uint_as_float(uint32_t(127 + Fmt::kShift - kept) << 23);
+  if (a >= 0x7f800000u) {
+    g.scale = 255u;
+    g.factor = 0.0f;
+    g.top = true;
+  }
+  return g;
+}
+
+// Eight codes of a lane.
+struct Int8Fmt {
+  static constexpr uint32_t kLimitFraction = 0x7e0000u;  // 127/64 = 1.984375
+  static constexpr int kLimitExponent = 0;
+  static constexpr int kShift = 6;        // a code counts 64ths of the scale
+  static constexpr double kUnit = 0x1p-6;
+
+  // Adding 1.5 2^23 rounds to the nearest whole number, ties to even, and
+  // leaves it as the low byte of the sum's bits (x factor is exact: a power
+  // of two).
+  __device__ __forceinline__ static u32x2 encode(const float (&x)[8], const Group &g) {
+    uint32_t t[8];
+    if (__builtin_expect(__ballot(g.top) != 0ull, 0)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float v = g.factor == 0.0f ? 0.0f : fminf(fmaxf(x[i] * g.factor, -127.0f), 127.0f);
+        t[i] = __float_as_uint(v + 0x1.8p23f);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t[i] = __float_as_uint(fmaf(x[i], g.factor, 0x1.8p23f));
+    }
+    u32x2 r;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t lo = __builtin_amdgcn_perm(t[4 * h + 1], t[4 * h], 0x0c0c0400u);
+      const uint32_t hi = __builtin_amdgcn_perm(t[4 * h + 3], t[4 * h + 2], 0x04000c0cu);
+      r[h] = lo | hi;
+    }
+    return r;
+  }
+
+  __device__ __forceinline__ static void decode(u32x2 v, float (&q)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = float(int32_t(v[i >> 2] << (24 - 8 * (i & 3))) >> 24);
+  }
+};
+
+struct E4m3Fmt {
+  static constexpr uint32_t kLimitFraction = 0x600000u;  // 448 = 1.75 2^8
+  static constexpr int kLimitExponent = 8;
+  static constexpr int kShift = 0;
+  static constexpr double kUnit = 1.0;
+
+  __device__ __forceinline__ static u32x2 encode(const float (&x)[8], const Group &g) {
+    float v[8];
+    if (__builtin_expect(__ballot(g.top) != 0ull, 0)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = g.factor == 0.0f ? 0.0f : x[i] * g.factor;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = x[i] * g.factor;
+    }
+    u32x2 r;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      int p = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h], v[4 * h + 1], 0, false);
+      p = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h + 2], v[4 * h + 3], p, true);
+      r[h] = uint32_t(p);
+    }
+    return r;
+  }
+
+  __device__ __forceinline__ static void decode(u32x2 v, float (&q)[8]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(int(v[h]), false);
+      const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(int(v[h]), true);
+      q[4 * h] = lo.x;
+      q[4 * h + 1] = lo.y;
+      q[4 * h + 2] = hi.x;
+      q[4 * h + 3] = hi.y;
+    }
+  }
+};
+
+// ---- eight source elements of a lane: their bits' largest magnitude, and
+// their values.  load_some() takes the first n of them and zeros.
+
+__device__ __forceinline__ uint32_t top_of_halves(u32x4 v) {
+  u16x2 m = __builtin_bit_cast(u16x2, v[0] & 0x7fff7fffu);
+#pragma unroll
+  for (int q = 1; q < 4; ++q)
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, v[q] & 0x7fff7fffu));
+  return max(uint32_t(m.x), uint32_t(m.y));
+}
+
+__device__ __forceinline__ u32x4 some_halves(const uint16_t *p, uint64_t n) {
+  uint16_t t[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) t[i] = uint64_t(i) < n ? p[i] : uint16_t(0);
+  u32x4 r;
+  memcpy(&r, t, 16);
+  return r;
+}
+
+struct Bf16Src {
+  using E = uint16_t;
+  using Raw = u32x4;
+  __device__ __forceinline__ static Raw load(const E *p) {
+    return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
+  }
+  __device__ __forceinline__ static Raw load_some(const E *p, uint64_t n) {
+    return some_halves(p, n);
+  }
+  __device__ __forceinline__ static uint32_t top(const Raw &v) { return top_of_halves(v); }
+  __device__ __forceinline__ static uint32_t magnitude(uint32_t t) { return t << 16; }
+  __device__ __forceinline__ static void values(const Raw &v, float (&x)[8]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      x[2 * q] = __uint_as_float(v[q] << 16);
+      x[2 * q + 1] = __uint_as_float(v[q] & 0xffff0000u);
+    }
+  }
+};
+
+struct F16Src {
+  using E = uint16_t;
+  using Raw = u32x4;
+  __device__ __forceinline__ static Raw load(const E *p) { return Bf16Src::load(p); }
+  __device__ __forceinline__ static Raw load_some(const E *p, uint64_t n) {
+    return some_halves(p, n);
+  }
+  __device__ __forceinline__ static uint32_t top(const Raw &v) { return top_of_halves(v); }
+  __device__ __forceinline__ static uint32_t magnitude(uint32_t t) {
+    return __float_as_uint(float(__builtin_bit_cast(_Float16, uint16_t(t))));
+  }
+  __device__ __forceinline__ static void values(const Raw &v, float (&x)[8]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      x[2 * q] = float(__builtin_bit_cast(_Float16, uint16_t(v[q])));
+      x[2 * q + 1] = float(__builtin_bit_cast(_Float16, uint16_t(v[q] >> 16)));
+    }
+  }
+};
+
+struct F32Src {
+  using E = float;
+  struct Raw {
+    u32x4 v[2];
+  };
+  __device__ __forceinline__ static Raw load(const E *p) {
+    const u32x4 *q = reinterpret_cast<const u32x4 *>(p);
+    return {{q[0], q[1]}};
+  }
+  __device__ __forceinline__ static Raw load_some(const E *p, uint64_t n) {
+    Raw r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.v[i >> 2][i & 3] = __float_as_uint(uint64_t(i) < n ? p[i] : 0.0f);
+    return r;
+  }
+  __device__ __forceinline__ static uint32_t top(const Raw &r) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, r.v[i >> 2][i & 3] & 0x7fffffffu);
+    return m;
+  }
+  __device__ __forceinline__ static uint32_t magnitude(uint32_t t) { return t; }
+  __device__ __forceinline__ static void values(const Raw &r, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(r.v[i >> 2][i & 3]);
+  }
+};
+
+}  // namespace cheb

@@ -1,0 +1,324 @@
+// Device kernels of the 8-bit history for gfx950 (CDNA4, wave64): a full
+// step quantised as it is stored, predictions from such entries, and the
+// residual update from them.  The entries' format is described with
+// cheb_cache_create_quant, their place in the arena in internal.h.
+#include <hip/hip_runtime.h>
+
+#include <stdint.h>
+#include <string.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "coded.h"
+#include "internal.h"
+#include "shapes.h"
+
+namespace cheb {
+namespace {
+
+// ---- full-step push ----------------------------------------------------------
+
+struct StoreArgs {
+  const void *src[kGatherSegs];
+  uint32_t block[kGatherSegs];  // first block in the entry
+  uint64_t numel[kGatherSegs];
+  GatherClass cls[kGatherClasses];
+  int32_t classes;
+  char *codes, *scales;
+  uint64_t code_super, scale_super;
+};
+
+constexpr int kRuns = int(kCodedBlock) / 512;   // runs of 64 lanes x 8 elements in a block
+constexpr int64_t kStoreVec = kCodedBlock / kGatherTileVecs;
+
+// One wave quantises a block of 4096 elements: eight runs of 64 lanes x 8
+// elements.  The four lanes of a group find its largest magnitude by two
+// exchanges; the eight runs' scales go out as one 128-byte line.
+template <class Fmt, class Src, bool kFlat>
+__global__ __launch_bounds__(64) void store_kernel(StoreArgs a) {
+  uint32_t s = blockIdx.y, tile = blockIdx.x;
+  if constexpr (!kFlat) {
+    int32_t p = 0;
+    for (int32_t q = 1; q < a.classes; ++q)
+      if (blockIdx.x >= a.cls[q].block) p = q;
+    const GatherClass c = a.cls[p];
+    const uint32_t b = blockIdx.x - c.block;
+    s = __umulhi(b, c.inverse);  // b / tiles, or one less
+    tile = b - s * c.tiles;
+    if (tile >= c.tiles) {
+      ++s;
+      tile -= c.tiles;
+    }
+    s += uint32_t(c.seg);
+  }
+  const uint64_t numel = a.numel[s];
+  const uint64_t first = uint64_t(tile) * uint64_t(kCodedBlock);
+  if (first >= numel) return;
+  const uint32_t lane = threadIdx.x;
+  const typename Src::E *src = static_cast<const typename Src::E *>(a.src[s]) + first + lane * 8u;
+  const uint32_t block = a.block[s] + tile;
+  char *codes = a.codes + uint64_t(block >> 3) * a.code_super + (block & 7u) * 4096u + lane * 8u;
+  char *scales = a.scales + uint64_t(block >> 3) * a.scale_super + (block & 7u) * 128u;
+  typename Src::Raw v[kRuns];
+  if (first + uint64_t(kCodedBlock) <= numel) {
+#pragma unroll
+    for (int r = 0; r < kRuns; ++r) v[r] = Src::load(src + r * 512);
+  } else {
+#pragma unroll
+    for (int r = 0; r < kRuns; ++r) {
+      const uint64_t at = first + uint64_t(r) * 512u + lane * 8u;
+      v[r] = Src::load_some(src + r * 512, at < numel ? numel - at : 0u);
+    }
+  }
+  __builtin_amdgcn_sched_barrier(0);
+  u32x2 scale = {0u, 0u};
+#pragma unroll
+  for (int r = 0; r < kRuns; ++r) {
+    const Group g = group_of<Fmt>(Src::magnitude(quad_max(Src::top(v[r]))));
+    float x[8];
+    Src::values(v[r], x);
+    __builtin_nontemporal_store(Fmt::encode(x, g), reinterpret_cast<u32x2 *>(codes + r * 512));
+    scale[r >> 2] |= g.scale << ((r & 3) * 8);
+  }
+  if ((lane & 3u) == 0) *reinterpret_cast<u32x2 *>(scales + (lane >> 2) * 8u) = scale;
+}
+
+template <class Fmt, class Src>
+hipError_t launch_store_typed(const StoreArgs &a, const GatherPlan &plan, hipStream_t s) {
+  const dim3 grid = plan.flat ? dim3(plan.widest, uint32_t(plan.segs)) : dim3(plan.blocks);
+  const auto kernel = plan.flat ? store_kernel<Fmt, Src, true> : store_kernel<Fmt, Src, false>;
+  hipLaunchKernelGGL(kernel, grid, dim3(64), 0, s, a);
+  return hipGetLastError();
+}
+
+template <class Fmt>
+hipError_t launch_store_fmt(int dtype, const StoreArgs &a, const GatherPlan &plan, hipStream_t s) {
+  switch (dtype) {
+    case CHEB_BF16: return launch_store_typed<Fmt, Bf16Src>(a, plan, s);
+    case CHEB_F16: return launch_store_typed<Fmt, F16Src>(a, plan, s);
+    default: return launch_store_typed<Fmt, F32Src>(a, plan, s);
+  }
+}
+
+// ---- residual update ---------------------------------------------------------
+
+constexpr int kCover = 128;
+
+struct CodedPart {
+  uint32_t tile;
+  uint32_t vec_begin, n_vec;
+  int32_t first, ncover;  // its covering segments in the delta table
+};
+
+template <int NS>
+struct CodedResArgs {
+  const char *codes[NS], *scales[NS];
+  float w[NS];
+  int64_t delta[kCover];  // vectors of 8, from an entry's start to the segment's residual vector 0
+  CodedPart part[kMaxResIntervals];
+  int32_t n_part;
+  uint32_t code_super, scale_super;
+  const float *x_in;  // may be null: zero
+  float *x_out;
+};
+
+// A tile is a run of 64 residual vectors of 8.  The W waves of a block share
+// it, each taking every W-th batch of U covering segments.  A segment's
+// entries are summed in fp32 (at most 8 terms), segments in fp64.
+template <class Fmt, int NS, int W, int U>
+__global__ __launch_bounds__(64 * W) void residual_coded_kernel(CodedResArgs<NS> a) {
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t lane = threadIdx.x & 63u;
+  int32_t p = 0;
+  for (int32_t q = 1; q < a.n_part; ++q)
+    if (blockIdx.x >= a.part[q].tile) p = q;
+  const CodedPart part = a.part[p];
+  const uint32_t first = (blockIdx.x - part.tile) * 64u;
+  const uint32_t live = std::min(part.n_vec - first, 64u);
+  const uint32_t l = lane < live ? lane : live - 1u;  // idle lanes repeat the last
+  const uint64_t j0 = uint64_t(part.vec_begin) + first;
+  double acc[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = -0.0;  // the sum of nothing: x + -0.0 is x, -0.0 too
+  auto take = [&](auto count, int32_t at) {
+    constexpr int N = decltype(count)::value;
+    u32x2 v[N][NS];
+    uint32_t sc[N][NS];
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const uint64_t v0 = uint64_t(a.delta[part.first + at + u]) + j0;
+      const uint64_t chunk = v0 >> 12;
+      uint32_t r = (uint32_t(v0) & 4095u) + l;
+      const bool next = r >= 4096u;  // 64 vectors span at most two chunks
+      r &= 4095u;
+      const uint32_t co = r * 8u + (next ? a.code_super : 0u);
+      const uint32_t so = (r >> 9) * 128u + (r >> 2 & 15u) * 8u + (r >> 6 & 7u) +
+                          (next ? a.scale_super : 0u);
+#pragma unroll
+      for (int k = 0; k < NS; ++k) {
+        v[u][k] = __builtin_nontemporal_load(
+            reinterpret_cast<const u32x2 *>(a.codes[k] + chunk * a.code_super + co));
+        sc[u][k] = *reinterpret_cast<const uint8_t *>(a.scales[k] + chunk * a.scale_super + so);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      float t[8];
+#pragma unroll
+      for (int k = 0; k < NS; ++k) {
+        const float unit = a.w[k] * __uint_as_float(sc[u][k] << 23);
+        float q[8];
+        Fmt::decode(v[u][k], q);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] = k == 0 ? unit * q[e] : fmaf(unit, q[e], t[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += double(t[e]);
+    }
+  };
+  int32_t c = int32_t(wave) * U;
+  for (; c + U <= part.ncover; c += W * U) take(std::integral_constant<int, U>(), c);
+  if constexpr (U > 1) {
+    for (; c < part.ncover; ++c) take(std::integral_constant<int, 1>(), c);
+  }
+  if constexpr (W == 1) {
+    if (lane >= live) return;
+    const uint64_t o = (j0 + lane) * 8u;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      u32x4 x = {0u, 0u, 0u, 0u}, r;
+      if (a.x_in) x = *reinterpret_cast<const u32x4 *>(a.x_in + o + 4 * h);
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        r[q] = __float_as_uint(float(double(__uint_as_float(x[q])) + acc[4 * h + q]));
+      *reinterpret_cast<u32x4 *>(a.x_out + o + 4 * h) = r;
+    }
+  } else {
+    // Element e of vector n at [e * 64 + n]: consecutive lanes write
+    // consecutive words.
+    __shared__ double sums[W][8 * 64];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[wave][e * 64 + int(lane)] = acc[e];
+    __syncthreads();
+    for (uint32_t h = threadIdx.x; h < live * 2u; h += 64u * W) {
+      const uint64_t o = j0 * 8u + 4u * h;
+      const uint32_t at = (4u * (h & 1u)) * 64u + (h >> 1);
+      u32x4 x = {0u, 0u, 0u, 0u}, r;
+      if (a.x_in) x = *reinterpret_cast<const u32x4 *>(a.x_in + o);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        double s = double(__uint_as_float(x[q]));
+#pragma unroll
+        for (int w = 0; w < W; ++w) s += sums[w][at + uint32_t(q) * 64u];
+        r[q] = __float_as_uint(float(s));
+      }
+      *reinterpret_cast<u32x4 *>(a.x_out + o) = r;
+    }
+  }
+}
+
+struct CodedResJob {
+  const CodedEntry *src;
+  const double *w;
+  const int64_t *delta;
+  int n_delta;
+  const ResidualInterval *iv;
+  int n_iv;
+  const float *x_in;
+  float *x_out;
+  const CodedPlace *place;
+  int cus;
+};
+
+template <class Fmt, int NS>
+hipError_t launch_residual_ns(const CodedResJob &j, hipStream_t s) {
+  CodedResArgs<NS> a;
+  memset(&a, 0, sizeof a);
+  for (int k = 0; k < NS; ++k) {
+    a.codes[k] = j.src[k].codes;
+    a.scales[k] = j.src[k].scales;
+    a.w[k] = float(j.w[k] * Fmt::kUnit);
+  }
+  memcpy(a.delta, j.delta, sizeof(int64_t) * size_t(j.n_delta));
+  a.code_super = uint32_t(j.place->code_super);
+  a.scale_super = uint32_t(j.place->scale_super);
+  a.x_in = j.x_in;
+  a.x_out = j.x_out;
+  a.n_part = j.n_iv;
+  uint32_t tiles = 0;
+  int ncover = 0;
+  for (int i = 0, first = 0; i < j.n_iv; first += j.iv[i].ncover, ++i) {
+    const uint32_t n_vec = uint32_t(j.iv[i].n_vec);
+    a.part[i] = CodedPart{tiles, uint32_t(j.iv[i].vec_begin), n_vec, first, j.iv[i].ncover};
+    tiles += (n_vec + 63u) / 64u;
+    ncover = std::max(ncover, int(j.iv[i].ncover));
+  }
+  constexpr int U = NS <= 2 ? 4 : NS <= 4 ? 2 : 1;
+  if (ncover >= 8)
+    hipLaunchKernelGGL((residual_coded_kernel<Fmt, NS, 4, U>), dim3(tiles), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((residual_coded_kernel<Fmt, NS, 1, U>), dim3(tiles), dim3(64), 0, s, a);
+  return hipGetLastError();
+}
+
+template <class Fmt>
+hipError_t launch_residual_fmt(int n, const CodedResJob &j, hipStream_t s) {
+  switch (n) {
+    case 1: return launch_residual_ns<Fmt, 1>(j, s);
+    case 2: return launch_residual_ns<Fmt, 2>(j, s);
+    case 3: return launch_residual_ns<Fmt, 3>(j, s);
+    case 4: return launch_residual_ns<Fmt, 4>(j, s);
+    case 5: return launch_residual_ns<Fmt, 5>(j, s);
+    case 6: return launch_residual_ns<Fmt, 6>(j, s);
+    case 7: return launch_residual_ns<Fmt, 7>(j, s);
+    default: return launch_residual_ns<Fmt, 8>(j, s);
+  }
+}
+
+}  // namespace
+
+int launch_store(int quant, int dtype, const CodedEntry &to, const CodedPlace &place,
+                 GatherSeg *segs, int n_segs, hipStream_t stream) {
+  n_segs = order_segments(segs, n_segs);
+  StoreArgs a;
+  for (int at = 0; at < n_segs;) {
+    // Blocks of 4096 elements: 64 "vectors" of 64.
+    const GatherPlan plan = next_gather(segs + at, n_segs - at, kStoreVec, kChunkVecs);
+    memset(&a, 0, sizeof a);
+    for (int j = 0; j < plan.segs; ++j) {
+      a.src[j] = segs[at + j].src;
+      a.block[j] = uint32_t(segs[at + j].dst_offset / kCodedBlock);
+      a.numel[j] = uint64_t(segs[at + j].numel);
+    }
+    memcpy(a.cls, plan.cls, sizeof(GatherClass) * size_t(plan.classes));
+    a.classes = plan.classes;
+    a.codes = const_cast<char *>(to.codes);
+    a.scales = const_cast<char *>(to.scales);
+    a.code_super = place.code_super;
+    a.scale_super = place.scale_super;
+    at += plan.segs;
+    const hipError_t e = quant == CHEB_QUANT_MXINT8
+                             ? launch_store_fmt<Int8Fmt>(dtype, a, plan, stream)
+                             : launch_store_fmt<E4m3Fmt>(dtype, a, plan, stream);
+    if (e != hipSuccess) return fail(CHEB_E_HIP, "push launch failed: %s", hipGetErrorString(e));
+  }
+  return ok();
+}
+
+int launch_residual_coded(int quant, int n, const CodedEntry *src, const double *w,
+                          const int64_t *delta, int n_delta, const ResidualInterval *iv, int n_iv,
+                          const float *x_in, float *x_out, const CodedPlace &place,
+                          hipStream_t stream) {
+  CodedResJob j{src, w, delta, n_delta, iv, n_iv, x_in, x_out, &place, 0};
+  int lds = 0;
+  int rc = device_info(&j.cus, &lds);
+  if (rc != CHEB_OK) return rc;
+  const hipError_t e = quant == CHEB_QUANT_MXINT8 ? launch_residual_fmt<Int8Fmt>(n, j, stream)
+                                                  : launch_residual_fmt<E4m3Fmt>(n, j, stream);
+  if (e != hipSuccess) return fail(CHEB_E_HIP, "residual launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+}  // namespace cheb

@@ -60,6 +60,11 @@ int weights_row(const double *x, int n, double target, double *w);
 int launch_combine(int dtype, const void *const *src, int n, const double *w, int n_out,
                    void *const *out, int64_t numel, int64_t super_vecs, hipStream_t stream);
 
+// The checks of a combination's or prediction's counts and weights, and of its
+// outputs (numel > 0).  CHEB_OK, or the error with its message.
+int check_weights(const double *w, int32_t n_src, int32_t n_out, int64_t numel, int32_t dtype);
+int check_outputs(int32_t n_out, void *const *out, int64_t numel, int32_t dtype);
+
 // Validation of cheb_combine_multi's arguments followed by launch_combine.
 int combine_checked(const void *const *src, int32_t n_src, const double *w, int32_t n_out,
                     void *const *out, int64_t numel, int32_t dtype, int64_t super_vecs,
@@ -107,10 +112,55 @@ inline int64_t gather_lead(int64_t dst_vec, bool whole) {
   return whole ? dst_vec % kGatherTileVecs : 0;
 }
 
+// ---- 8-bit entries ----------------------------------------------------------
+//
+// An entry of a ring made by cheb_cache_create_quant holds one code byte an
+// element, in order, and one E8M0 scale byte for each group of 32.  Cached
+// tensors start on blocks of kCodedBlock elements, so a block (4 KiB of codes,
+// a 128-byte line of scales) belongs to one tensor.  Both are cut into chunks
+// of kCodedChunk elements: element e has its code at
+//     codes + (e >> kCodedChunkLg) * code_super + e % kCodedChunk
+// and its scale at
+//     scales + (e >> kCodedChunkLg) * scale_super + coded_scale(e % kCodedChunk),
+// coded_scale(r) = (r >> 12) * 128 + (r >> 5 & 15) * 8 + (r >> 9 & 7): the four
+// lanes of a wave that hold a group (8 elements each, 512 a run) find that
+// group's place in all eight runs of a block side by side, so that several
+// runs' scales are one load or store.
+constexpr int kCodedBlockLg = 12, kCodedChunkLg = 15, kCodedVec = 8;
+constexpr int64_t kCodedBlock = int64_t(1) << kCodedBlockLg;
+constexpr int64_t kCodedChunk = int64_t(1) << kCodedChunkLg;
+constexpr int64_t kCodedChunkScales = kCodedChunk / 32;
+
+// Where the entries' codes and scales lie: slot j's at codes + j * code_lane
+// and scales + j * scale_lane.
+struct CodedPlace {
+  char *codes = nullptr, *scales = nullptr;
+  size_t code_lane = 0, scale_lane = 0;
+  size_t code_super = 0, scale_super = 0;
+};
+
+// One entry's.
+struct CodedEntry {
+  const char *codes, *scales;
+};
+
+// Quantises one step's segments into the entry (coded.hip): the whole blocks
+// of each, zeros past its elements.  dst_offset is in elements from the
+// entry's start.  Reorders `segs`.
+int launch_store(int quant, int dtype, const CodedEntry &to, const CodedPlace &place,
+                 GatherSeg *segs, int n_segs, hipStream_t stream);
+
+// out[m][i] = sum_k w[m * n + k] * value_k[i], i < numel, a whole number of
+// blocks.
+int launch_predict_coded(int quant, int dtype, const CodedEntry *src, int n, const double *w,
+                         int n_out, void *const *out, int64_t numel, const CodedPlace &place,
+                         hipStream_t stream);
+
 // Read-only view of a cache's layout and ring state (cache.cpp).
 struct CacheView {
   int32_t n_slots, dtype, count, n_segs, layout;
   bool push_open;
+  const struct CodedOps *coded;  // null: plain entries
   const int64_t *seg_numel, *seg_offset;
   int64_t slot_numel;
   int64_t super_vecs;  // kChunkVecs for the slot layout
@@ -142,5 +192,12 @@ int launch_residual_intervals(int dtype, int n, const uint64_t *base, const doub
                               const int64_t *delta, int n_delta, const ResidualInterval *iv,
                               int n_iv, const float *x_in, float *x_out, int64_t super_vecs,
                               hipStream_t stream);
+
+// The same from 8-bit entries, delta and vec_begin in vectors of kCodedVec
+// elements.
+int launch_residual_coded(int quant, int n, const CodedEntry *src, const double *w,
+                          const int64_t *delta, int n_delta, const ResidualInterval *iv, int n_iv,
+                          const float *x_in, float *x_out, const CodedPlace &place,
+                          hipStream_t stream);
 
 }  // namespace cheb

@@ -11,7 +11,7 @@
 #include <algorithm>
 #include <vector>
 
-#include "internal.h"
+#include "cache.h"
 
 using namespace cheb;
 
@@ -75,11 +75,10 @@ int check_residual_buffers(const float *x_in, float *x_out, int64_t res_numel) {
 // tables, it is one launch, the largest interval first, so that the chip does
 // not run empty between them.  Otherwise, per interval, the covering segments
 // in chunks of the table's size; the first chunk reads x_in, later ones x_out.
-template <class DeltaFn>
-int run(int dtype, int n, const uint64_t *base, const double *w,
-        const std::vector<Interval> &plan_iv, DeltaFn delta_of, const float *x_in, float *x_out,
-        int64_t super_vecs, hipStream_t stream) {
-  const int vec = elems_per_vec(dtype);
+// launch(delta, n_delta, intervals, n_intervals, x_in) enqueues one of them.
+template <class DeltaFn, class LaunchFn>
+int run(const std::vector<Interval> &plan_iv, int vec, DeltaFn delta_of, const float *x_in,
+        const float *x_out, LaunchFn launch) {
   const size_t max_cover = size_t(residual_max_cover());
   std::vector<int64_t> delta;
   size_t covers = 0;
@@ -99,24 +98,32 @@ int run(int dtype, int n, const uint64_t *base, const double *w,
       parts[i] = {iv.begin / vec, (iv.end - iv.begin) / vec, int32_t(iv.segs.size())};
       for (int32_t s : iv.segs) delta.push_back(delta_of(s));
     }
-    return launch_residual_intervals(dtype, n, base, w, delta.data(), int(covers), parts, n_parts,
-                                     x_in, x_out, super_vecs, stream);
+    return launch(delta.data(), int(covers), parts, n_parts, x_in);
   }
   for (const Interval &iv : plan_iv) {
-    const int64_t vb = iv.begin / vec, nv = (iv.end - iv.begin) / vec;
     size_t first = 0;
     do {
       const size_t count = std::min(iv.segs.size() - first, max_cover);
       delta.assign(count, 0);
       for (size_t c = 0; c < count; ++c) delta[c] = delta_of(iv.segs[first + c]);
-      const float *in = first == 0 ? x_in : x_out;
-      int rc = launch_residual(dtype, n, base, w, delta.data(), int(count), in, x_out, vb, nv,
-                               super_vecs, stream);
+      const ResidualInterval part{iv.begin / vec, (iv.end - iv.begin) / vec, int32_t(count)};
+      int rc = launch(delta.data(), int(count), &part, 1, first == 0 ? x_in : x_out);
       if (rc != CHEB_OK) return rc;
       first += count;
     } while (first < iv.segs.size());
   }
   return ok();
+}
+
+// The launches of plain entries.
+int launch_plain(int dtype, int n, const uint64_t *base, const double *w, const int64_t *delta,
+                 int n_delta, const ResidualInterval *iv, int n_iv, const float *x_in,
+                 float *x_out, int64_t super_vecs, hipStream_t stream) {
+  if (n_iv == 1)
+    return launch_residual(dtype, n, base, w, delta, n_delta, x_in, x_out, iv->vec_begin,
+                           iv->n_vec, super_vecs, stream);
+  return launch_residual_intervals(dtype, n, base, w, delta, n_delta, iv, n_iv, x_in, x_out,
+                                   super_vecs, stream);
 }
 
 }  // namespace
@@ -140,8 +147,19 @@ int cheb_residual_apply(cheb_cache *c, const double *w, const int64_t *res_offse
   if (o < a + v.arena_bytes && a < o + uintptr_t(res_numel) * 4u)
     return fail(CHEB_E_INVAL, "x_out overlaps the cache arena");
   std::vector<Interval> iv;
-  rc = plan(v.seg_numel, res_offset, v.n_segs, res_numel, elems_per_vec(v.dtype), &iv);
+  const int vec = v.coded ? kCodedVec : elems_per_vec(v.dtype);
+  rc = plan(v.seg_numel, res_offset, v.n_segs, res_numel, vec, &iv);
   if (rc != CHEB_OK) return rc;
+  // Vectors from the entry base to the segment's vector of residual vector 0
+  // (both offsets are whole vectors; the kernel places each by its chunk).
+  auto delta_of = [&](int32_t s) { return (v.seg_offset[s] - res_offset[s]) / vec; };
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (v.coded)
+    return run(iv, vec, delta_of, x_in, x_out,
+               [&](const int64_t *delta, int n_delta, const ResidualInterval *parts, int n_parts,
+                   const float *in) {
+                 return v.coded->residual(c, w, delta, n_delta, parts, n_parts, in, x_out, s);
+               });
   uint64_t base[CHEB_MAX_SLOTS];
   for (int32_t k = 0; k < v.n_slots; ++k) {
     void *p = nullptr;
@@ -149,12 +167,12 @@ int cheb_residual_apply(cheb_cache *c, const double *w, const int64_t *res_offse
     if (rc != CHEB_OK) return rc;
     base[k] = reinterpret_cast<uint64_t>(p);
   }
-  // Vectors from the entry base to the segment's vector of residual vector 0
-  // (both offsets are whole vectors; the kernel places each by its chunk).
-  const int64_t vec = elems_per_vec(v.dtype);
-  auto delta_of = [&](int32_t s) { return (v.seg_offset[s] - res_offset[s]) / vec; };
-  return run(v.dtype, v.n_slots, base, w, iv, delta_of, x_in, x_out, v.super_vecs,
-             static_cast<hipStream_t>(stream));
+  return run(iv, vec, delta_of, x_in, x_out,
+             [&](const int64_t *delta, int n_delta, const ResidualInterval *parts, int n_parts,
+                 const float *in) {
+               return launch_plain(v.dtype, v.n_slots, base, w, delta, n_delta, parts, n_parts, in,
+                                   x_out, v.super_vecs, s);
+             });
 }
 
 int cheb_residual_reduce(const void *const *seg_src, const int64_t *seg_numel,
@@ -175,14 +193,18 @@ int cheb_residual_reduce(const void *const *seg_src, const int64_t *seg_numel,
   rc = plan(seg_numel, res_offset, n_segs, res_numel, elems_per_vec(dtype), &iv);
   if (rc != CHEB_OK) return rc;
   // Vectors from address 0 (the sources are 16-byte aligned).
-  const int64_t vec = elems_per_vec(dtype);
+  const int vec = elems_per_vec(dtype);
   const uint64_t base[1] = {0};
   const double one[1] = {1.0};
   auto delta_of = [&](int32_t s) {
     return int64_t(reinterpret_cast<uintptr_t>(seg_src[s]) / 16) - res_offset[s] / vec;
   };
-  return run(dtype, 1, base, one, iv, delta_of, x_in, x_out, kChunkVecs,
-             static_cast<hipStream_t>(stream));
+  return run(iv, vec, delta_of, x_in, x_out,
+             [&](const int64_t *delta, int n_delta, const ResidualInterval *parts, int n_parts,
+                 const float *in) {
+               return launch_plain(dtype, 1, base, one, delta, n_delta, parts, n_parts, in, x_out,
+                                   kChunkVecs, static_cast<hipStream_t>(stream));
+             });
 }
 
 }  // extern "C"
