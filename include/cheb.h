@@ -585,6 +585,87 @@ CHEB_API int cheb_residual_reduce(const void *const *seg_src, const int64_t *seg
                                   void *stream);
 
 /* ------------------------------------------------------------------------ */
+/* The residual's addition and the norm that follows it.                     */
+/* ------------------------------------------------------------------------ */
+
+/* What reads the residual stream after a skipped step's update, a following
+ * block that is computed or the final layer, normalises it first.  These calls
+ * form the updated residual and its norm in one pass.  For each of `rows` rows
+ * of `dim` elements:
+ *     x = x_in + sum_k w_k s_k                     (fp64, rounded to fp32)
+ *     h = x - mean(x)   (CHEB_NORM_LAYER), x       (CHEB_NORM_RMS)
+ *     y = h / sqrt(mean(h^2) + eps) * gain + shift
+ * x_out receives x rounded to x_dtype; y is formed from x before that rounding,
+ * its means in fp64, the rest in fp32, and rounded once to out_format. */
+enum { CHEB_NORM_RMS = 0, CHEB_NORM_LAYER = 1 };
+
+/* Output formats of y besides the storage types, both of e4m3 codes:
+ *   CHEB_OUT_MXFP8    one E8M0 scale byte for each 32 elements of a row (fewer
+ *                     in a row's last group), chosen and rounded as
+ *                     CHEB_QUANT_MXFP8's: what scaled matrix instructions take.
+ *                     y_scale [rows][ceil(dim / 32)].  A group with a NaN or an
+ *                     infinity has scale 255 (NaN) and codes 0.
+ *   CHEB_OUT_FP8_ROW  one fp32 scale a row, max|y| / 448 (1 for a row of zeros,
+ *                     at least 2^-126), codes y / scale rounded to nearest even.
+ *                     y_scale [rows].  A row with a NaN or an infinity has a NaN
+ *                     scale and codes 0. */
+enum { CHEB_OUT_MXFP8 = 16, CHEB_OUT_FP8_ROW = 17 };
+
+/* Largest row the norm calls take. */
+#define CHEB_MAX_NORM_DIM 16384
+
+/* The rows, their residual and the norm.  All pointers are device memory,
+ * aligned to their elements; arrays are contiguous.
+ *   rows, dim        rows >= 0, 1 <= dim <= CHEB_MAX_NORM_DIM; rows * dim below
+ *                    2^34, rows below 2^26.
+ *   kind             CHEB_NORM_RMS or CHEB_NORM_LAYER.
+ *   x_dtype          cheb_dtype of x_in and x_out.
+ *   eps              finite, >= 0.
+ *   x_in             [rows][dim], or NULL (zero).
+ *   x_out            [rows][dim], or NULL (x is not kept).  It may be x_in.
+ *   gain, shift      fp32 [groups][dim], each may be NULL (one, zero); row r
+ *                    takes group r / rows_per_group (an adaptive norm's per-image
+ *                    rows; rows_per_group = rows for one group).
+ *   rows_per_group   >= 1 where gain or shift is given.
+ *   out_format       a cheb_dtype, CHEB_OUT_MXFP8 or CHEB_OUT_FP8_ROW.
+ *   y                [rows][dim] elements of the storage type, or codes.
+ *   y_scale          scale bytes or fp32 scales; NULL for a storage type.
+ * x_out, y and y_scale overlap nothing else of the call. */
+typedef struct cheb_norm {
+  int64_t rows, dim;
+  double eps;
+  const void *x_in;
+  void *x_out;
+  const float *gain, *shift;
+  int64_t rows_per_group;
+  void *y, *y_scale;
+  int32_t kind, x_dtype, out_format;
+} cheb_norm;
+
+/* Sources s_k given by the caller: module outputs, or a residual branch with
+ * weight 1.
+ *   src  [n_src] host array of device pointers, each to rows * dim elements of
+ *        `dtype`, aligned to them.  0 <= n_src <= CHEB_MAX_SLOTS; with none,
+ *        src and w may be NULL and x_in is the norm's input.
+ *   w    [n_src] host fp64, finite.
+ * Errors: CHEB_E_INVAL (also neither sources nor x_in), CHEB_E_DTYPE,
+ * CHEB_E_ALIGN, CHEB_E_NONFINITE, CHEB_E_HIP. */
+CHEB_API int cheb_add_norm(const void *const *src, int32_t n_src, const double *w, int32_t dtype,
+                           const cheb_norm *norm, void *stream);
+
+/* Sources s_k from the history: elements first .. first + rows * dim - 1 of
+ * cached tensor `seg` of every held entry, oldest to newest (the predicted
+ * output of that module, or with a collapsed history the block stack's whole
+ * contribution).  Any cache, of either layout and of 8-bit entries too.
+ *   w    [n_slots] host fp64, aligned with cheb_cache_history.
+ * Requires a full history.  x equals cheb_residual_apply's result over a cache
+ * of fp32, bf16 or fp16 entries with that one segment, bit for bit, where
+ * x_dtype is CHEB_F32.  Errors: CHEB_E_INVAL (also a range past the tensor),
+ * CHEB_E_NOTREADY, CHEB_E_DTYPE, CHEB_E_ALIGN, CHEB_E_NONFINITE, CHEB_E_HIP. */
+CHEB_API int cheb_residual_norm(cheb_cache *c, const double *w, int32_t seg, int64_t first,
+                                const cheb_norm *norm, void *stream);
+
+/* ------------------------------------------------------------------------ */
 /* Launch shape (tuning).                                                    */
 /* ------------------------------------------------------------------------ */
 

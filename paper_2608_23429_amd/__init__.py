@@ -16,7 +16,8 @@ from ._binding import (  # noqa: F401  (re-exported C entry points)
     CHEB_LAYOUT_INTERLEAVED, CHEB_LAYOUT_SLOTS, cheb_cache_arena_bytes_ex, cheb_cache_create_ex,
     cheb_cache_geometry, DEFAULT_LAUNCH_CONFIG, CHEB_QUANT_MXFP8, CHEB_QUANT_MXINT8,
     CHEB_QUANT_NONE, cheb_cache_create_quant, cheb_cache_layout_quant, cheb_cache_quant,
-    cheb_cache_read,
+    cheb_cache_read, cheb_add_norm, cheb_norm, cheb_residual_norm, CHEB_MAX_NORM_DIM,
+    CHEB_NORM_LAYER, CHEB_NORM_RMS, CHEB_OUT_FP8_ROW, CHEB_OUT_MXFP8,
     CHEB_BF16, CHEB_F16, CHEB_F32, CHEB_MAX_NODES, CHEB_MAX_OUTPUTS, CHEB_MAX_SLOTS, CHEB_RHO_ALTERNATING,
     CHEB_RHO_GENERAL, CHEB_SHORT_FULL, CHEB_TAYLOR, CHEB_SHORT_LOWER, ChebError, cheb_chebyshev_nodes,
     cheb_precompute_weights_variant,
@@ -195,6 +196,112 @@ def residual_reduce(segments: Sequence[torch.Tensor], res_offset, x_out: torch.T
     return x_out
 
 
+_NORMS = {"rms": CHEB_NORM_RMS, "layer": CHEB_NORM_LAYER}
+_OUT_8BIT = {"mxfp8": CHEB_OUT_MXFP8, "fp8_row": CHEB_OUT_FP8_ROW}
+
+
+def norm_output(rows: int, dim: int, out=torch.bfloat16, device=None):
+    """Buffers for a norm's output: a [rows, dim] tensor for a torch type, or
+    for "mxfp8" and "fp8_row" the e4m3 codes and their scales, [rows,
+    ceil(dim / 32)] powers of two or [rows] fp32."""
+    device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
+    if isinstance(out, torch.dtype):
+        cheb_dtype(out)
+        return torch.empty(rows, dim, dtype=out, device=device)
+    if out not in _OUT_8BIT:
+        raise ChebError(_binding.CHEB_E_DTYPE, f"unknown output format {out!r}")
+    y = torch.empty(rows, dim, dtype=torch.float8_e4m3fn, device=device)
+    if out == "fp8_row":
+        return y, torch.empty(rows, dtype=torch.float32, device=device)
+    return y, torch.empty(rows, -(-dim // 32), dtype=torch.float8_e8m0fnu, device=device)
+
+
+def _norm_call(tensors, x_out, x_in, numel, dim, kind, eps, gain, shift, out):
+    """The norm's structure and its output's buffers; every tensor of the call
+    is checked, and lies on the current device."""
+    for t, what in ((x_out, "x_out"), (x_in, "x_in"), (gain, "gain"), (shift, "shift")):
+        if t is not None:
+            _check_device_tensor(t, what)
+    x = x_in if x_in is not None else x_out
+    if x_in is not None and x_out is not None and (x_in.dtype != x_out.dtype
+                                                   or x_in.numel() != x_out.numel()):
+        raise ChebError(_binding.CHEB_E_MISMATCH, "x_in differs from x_out")
+    if x is not None and x.numel() != numel:
+        raise ChebError(_binding.CHEB_E_MISMATCH, f"the residual holds {x.numel()} elements, "
+                        f"the sources {numel}")
+    dim = int(dim)
+    if dim < 1 or numel % dim:
+        raise ChebError(_binding.CHEB_E_MISMATCH, f"{numel} elements are no rows of {dim}")
+    if kind not in _NORMS:
+        raise ChebError(_binding.CHEB_E_INVAL, f"unknown norm {kind!r}")
+    rows = numel // dim
+    groups = 0
+    for t, what in ((gain, "gain"), (shift, "shift")):
+        if t is None:
+            continue
+        if t.dtype is not torch.float32 or t.numel() == 0 or t.numel() % dim:
+            raise ChebError(_binding.CHEB_E_MISMATCH, f"{what} must be float32 rows of {dim}")
+        if groups not in (0, t.numel() // dim) or rows % (t.numel() // dim):
+            raise ChebError(_binding.CHEB_E_MISMATCH, f"{what}: {rows} rows in "
+                            f"{t.numel() // dim} groups, or not as many as the gain's")
+        groups = t.numel() // dim
+    if isinstance(out, (str, torch.dtype)):
+        device = tensors[0].device if tensors else x.device
+        out = norm_output(rows, dim, out, device)
+    y, scale = out if isinstance(out, tuple) else (out, None)
+    _check_device_tensor(y, "out")
+    if scale is None:
+        fmt = cheb_dtype(y.dtype)
+    else:
+        _check_device_tensor(scale, "out's scales")
+        fmt = CHEB_OUT_FP8_ROW if scale.dtype is torch.float32 else CHEB_OUT_MXFP8
+        want = rows if fmt == CHEB_OUT_FP8_ROW else rows * -(-dim // 32)
+        if (y.dtype is not torch.float8_e4m3fn or scale.numel() != want
+                or (fmt == CHEB_OUT_MXFP8 and scale.dtype is not torch.float8_e8m0fnu)):
+            raise ChebError(_binding.CHEB_E_MISMATCH, "out differs from norm_output's")
+    if y.numel() != numel:
+        raise ChebError(_binding.CHEB_E_MISMATCH, f"out holds {y.numel()} elements, not {numel}")
+    current = torch.cuda.current_device()
+    for t in (*tensors, x_out, x_in, gain, shift, y, scale):
+        if t is not None and t.device.index != current:
+            raise ChebError(_binding.CHEB_E_INVAL,
+                            f"a tensor is on {t.device}, the current device is {current}")
+    norm = cheb_norm(rows, dim, float(eps), None if x_in is None else x_in.data_ptr(),
+                     None if x_out is None else x_out.data_ptr(),
+                     None if gain is None else gain.data_ptr(),
+                     None if shift is None else shift.data_ptr(), rows // groups if groups else 0,
+                     y.data_ptr(), None if scale is None else scale.data_ptr(), _NORMS[kind],
+                     CHEB_F32 if x is None else cheb_dtype(x.dtype), fmt)
+    return norm, out
+
+
+def add_norm(srcs: Sequence[torch.Tensor], w, x_out: Optional[torch.Tensor] = None,
+             x_in: Optional[torch.Tensor] = None, *, dim: Optional[int] = None,
+             kind: str = "rms", eps: float = 1e-6, gain: Optional[torch.Tensor] = None,
+             shift: Optional[torch.Tensor] = None, out=torch.bfloat16,
+             stream: Optional[torch.cuda.Stream] = None):
+    """x = x_in + sum_k w[k] * srcs[k], kept in x_out if given, and its norm,
+    in one pass: (x_out, y).  ``kind`` is "rms" or "layer"; ``gain`` and
+    ``shift`` are fp32 [dim] or [groups, dim], each group for as many rows.
+    ``out`` names y's format (a torch type, "mxfp8", "fp8_row") or is
+    norm_output's buffers."""
+    if len(srcs) == 0 and x_in is None:
+        raise ChebError(_binding.CHEB_E_INVAL, "neither sources nor x_in")
+    like = srcs[0] if len(srcs) else x_in
+    _check_device_tensor(like, "srcs[0]" if len(srcs) else "x_in")
+    dtype, numel = like.dtype, like.numel()
+    dt = cheb_dtype(dtype)
+    for i, s in enumerate(srcs):
+        if not _plain(s, dtype, numel):
+            _check_device_tensor(s, f"srcs[{i}]")
+            raise ChebError(_binding.CHEB_E_MISMATCH, f"srcs[{i}] differs in dtype or size")
+    if dim is None:
+        dim = like.shape[-1] if like.dim() else 1
+    norm, out = _norm_call(srcs, x_out, x_in, numel, dim, kind, eps, gain, shift, out)
+    cheb_add_norm([s.data_ptr() for s in srcs], w, dt, norm, _stream_handle(stream))
+    return x_out, out
+
+
 class ResidualHistory:
     """Collapsed history: per full step, only the block stack's total
     contribution to the residual stream (fp32), in a ring of n entries.  A
@@ -249,6 +356,21 @@ class ResidualHistory:
         w = cheb_precompute_weights(self.history(), [target_t])[0]
         self.cache.residual_apply(w, [0], x_out, x_in, stream=stream)
         return x_out, w
+
+    def predict_norm(self, target_t: float, x_out: Optional[torch.Tensor] = None,
+                     x_in: Optional[torch.Tensor] = None, *, dim: int, first: int = 0,
+                     rows: Optional[int] = None, kind: str = "rms", eps: float = 1e-6,
+                     gain: Optional[torch.Tensor] = None, shift: Optional[torch.Tensor] = None,
+                     out=torch.bfloat16, stream: Optional[torch.cuda.Stream] = None):
+        """The skipped step's residual and its norm in one pass: (x_out, y, w).
+        Rows of ``dim`` from the residual's element ``first`` on: all of it, or
+        ``rows`` of them (the image tokens, say); x_in and x_out hold those.
+        Other arguments as add_norm's."""
+        w = cheb_precompute_weights(self.history(), [target_t])[0]
+        x_out, y = self.cache.residual_norm(w, 0, x_out, x_in, dim=dim, first=first, rows=rows,
+                                            kind=kind, eps=eps, gain=gain, shift=shift, out=out,
+                                            stream=stream)
+        return x_out, y, w
 
     def close(self):
         self.cache.close()
@@ -463,6 +585,28 @@ class ChebCache:
                             _stream_handle(stream))
         return x_out
 
+    def residual_norm(self, w, seg: int, x_out: Optional[torch.Tensor] = None,
+                      x_in: Optional[torch.Tensor] = None, *, dim: int, first: int = 0,
+                      rows: Optional[int] = None, kind: str = "rms", eps: float = 1e-6,
+                      gain: Optional[torch.Tensor] = None, shift: Optional[torch.Tensor] = None,
+                      out=torch.bfloat16, stream: Optional[torch.cuda.Stream] = None):
+        """x = x_in + the prediction of cached tensor ``seg`` from its element
+        ``first`` on, and its norm, in one pass: (x_out, y).  Rows of ``dim``,
+        as many as fit or ``rows``; other arguments as add_norm's."""
+        if not 0 <= seg < len(self.seg_numel):
+            raise ChebError(_binding.CHEB_E_INVAL, f"segment {seg} out of range")
+        w = np.asarray(w, dtype=np.float64).reshape(-1)
+        if w.size != self.n_slots:
+            raise ChebError(_binding.CHEB_E_INVAL, f"{w.size} weights for {self.n_slots} entries")
+        dim, left = int(dim), self.seg_numel[seg] - first
+        if dim < 1 or first < 0 or left < 0 or (rows is not None and rows < 0):
+            raise ChebError(_binding.CHEB_E_INVAL, f"no rows of {dim} from element {first} on")
+        rows = left // dim if rows is None else int(rows)
+        norm, out = _norm_call((self.arena,), x_out, x_in, rows * dim, dim, kind, eps, gain, shift,
+                               out)
+        cheb_residual_norm(self._h, w, seg, first, norm, _stream_handle(stream))
+        return x_out, out
+
     def extrapolate_at(self, target_t: float, out: Optional[torch.Tensor] = None,
                        stream: Optional[torch.cuda.Stream] = None):
         out = self.new_output() if out is None else out
@@ -473,5 +617,6 @@ class ChebCache:
 
 
 __all__ = [n for n in dir() if n.startswith("cheb_")] + [
-    "ChebCache", "ChebTable", "ChebError", "ResidualHistory", "residual_reduce", "combine", "combine_multi", "precompute_weights", "CHEB_BF16",
+    "ChebCache", "ChebTable", "ChebError", "ResidualHistory", "residual_reduce", "add_norm",
+    "norm_output", "combine", "combine_multi", "precompute_weights", "CHEB_BF16",
     "CHEB_F32", "CHEB_MAX_SLOTS", "CHEB_MAX_OUTPUTS", "CHEB_MAX_NODES", "LIB_PATH"]

@@ -41,6 +41,12 @@ CHEB_QUANT_NONE = 0
 CHEB_QUANT_MXINT8 = 1
 CHEB_QUANT_MXFP8 = 2
 
+CHEB_NORM_RMS = 0
+CHEB_NORM_LAYER = 1
+CHEB_OUT_MXFP8 = 16
+CHEB_OUT_FP8_ROW = 17
+CHEB_MAX_NORM_DIM = 16384
+
 CHEB_BF16 = 0
 CHEB_F32 = 1
 CHEB_F16 = 2
@@ -68,6 +74,15 @@ class cheb_launch_config(ctypes.Structure):
     _fields_ = [("block", ctypes.c_int32), ("unroll", ctypes.c_int32),
                 ("nontemporal", ctypes.c_int32), ("blocks_per_cu", ctypes.c_int32),
                 ("waves_per_cu", ctypes.c_int32)]
+
+
+class cheb_norm(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("dim", ctypes.c_int64), ("eps", ctypes.c_double),
+                ("x_in", ctypes.c_void_p), ("x_out", ctypes.c_void_p),
+                ("gain", ctypes.c_void_p), ("shift", ctypes.c_void_p),
+                ("rows_per_group", ctypes.c_int64), ("y", ctypes.c_void_p),
+                ("y_scale", ctypes.c_void_p), ("kind", ctypes.c_int32),
+                ("x_dtype", ctypes.c_int32), ("out_format", ctypes.c_int32)]
 
 
 # The library's launch shape at load time (64-lane blocks, occupancy capped by
@@ -140,6 +155,9 @@ SIGNATURES = {
     "cheb_residual_apply": [_vp, _dp, _i64p, ctypes.c_int64, _vp, _vp, _vp],
     "cheb_residual_reduce": [_vpp, _i64p, _i64p, ctypes.c_int32, ctypes.c_int32, _vp, _vp,
                              ctypes.c_int64, _vp],
+    "cheb_add_norm": [_vpp, ctypes.c_int32, _dp, ctypes.c_int32, ctypes.POINTER(cheb_norm), _vp],
+    "cheb_residual_norm": [_vp, _dp, ctypes.c_int32, ctypes.c_int64, ctypes.POINTER(cheb_norm),
+                           _vp],
     "cheb_get_launch_config": [ctypes.POINTER(cheb_launch_config)],
     "cheb_set_launch_config": [ctypes.POINTER(cheb_launch_config)],
 }
@@ -515,6 +533,21 @@ def cheb_residual_reduce(seg_ptrs, seg_numel, res_offset, dtype, x_in_ptr, x_out
     _check(LIB.cheb_residual_reduce(_voidp_array(seg_ptrs), sn, _i64ptr(res_offset)[0], n_segs,
                                     int(dtype), int(x_in_ptr or 0), int(x_out_ptr),
                                     int(res_numel), int(stream)))
+
+
+def cheb_add_norm(src_ptrs, w, dtype, norm, stream=0):
+    """norm: a cheb_norm structure."""
+    w = _f64(w).reshape(-1)
+    if w.size != len(src_ptrs):
+        raise ChebError(CHEB_E_INVAL, "one weight per source")
+    _check(LIB.cheb_add_norm(_voidp_array(src_ptrs), w.size, _dptr(w) if w.size else None,
+                             int(dtype), ctypes.byref(norm), int(stream)))
+
+
+def cheb_residual_norm(handle, w, seg, first, norm, stream=0):
+    w = _f64(w).reshape(-1)
+    _check(LIB.cheb_residual_norm(handle, _dptr(w), int(seg), int(first), ctypes.byref(norm),
+                                  int(stream)))
 
 
 def cheb_get_launch_config():

@@ -21,8 +21,9 @@ BUILD_DIR = os.path.join(ROOT, "_build", "cheb")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 ARCH = "gfx950"
 
-HOST_SOURCES = ["api.cpp", "cache.cpp", "table.cpp", "residual.cpp", "coded.cpp"]
-DEVICE_SOURCES = ["kernels.hip", "coded.hip", "predict_coded.hip"]
+HOST_SOURCES = ["api.cpp", "cache.cpp", "table.cpp", "residual.cpp", "coded.cpp",
+                "norm.cpp"]
+DEVICE_SOURCES = ["kernels.hip", "predict_coded.hip", "norm.hip", "coded.hip"]
 
 DEVICE_FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",

@@ -156,6 +156,23 @@ int launch_predict_coded(int quant, int dtype, const CodedEntry *src, int n, con
                          int n_out, void *const *out, int64_t numel, const CodedPlace &place,
                          hipStream_t stream);
 
+// The norm calls' sources (norm.hip): element e of source k is at base[k]
+// (plain entries: chunks of kChunkVecs vectors super_vecs apart, which is
+// contiguous memory where those are equal), or has its code and scale as the
+// entry src[k] says, `first` elements further on.
+struct NormSources {
+  int n = 0;
+  int dtype = CHEB_F32;         // of plain sources
+  int quant = CHEB_QUANT_NONE;  // else 8-bit entries
+  double w[CHEB_MAX_SLOTS];
+  const void *base[CHEB_MAX_SLOTS];
+  int64_t super_vecs = kChunkVecs;
+  CodedEntry src[CHEB_MAX_SLOTS];
+  CodedPlace place;
+  int64_t first = 0;
+};
+int launch_norm(const NormSources &from, const cheb_norm &norm, hipStream_t stream);
+
 // Read-only view of a cache's layout and ring state (cache.cpp).
 struct CacheView {
   int32_t n_slots, dtype, count, n_segs, layout;
