@@ -17,7 +17,7 @@ struct NormArgs {
   uint64_t base[CHEB_MAX_SLOTS], scales[CHEB_MAX_SLOTS];
   double w[CHEB_MAX_SLOTS];
   uint64_t first;                    // element of the sources' row 0
-  uint64_t super, scale_super;       // bytes from chunk to chunk
+  uint32_t super, scale_super;       // bytes from chunk to chunk
   int32_t n;
   int32_t chunked;                   // sources lie in chunks
   const void *x_in;
@@ -36,301 +36,474 @@ typedef u32x2 __attribute__((aligned(2))) half4_any;
 typedef u32x4 __attribute__((aligned(4))) float4_any;
 typedef uint32_t __attribute__((aligned(1))) code4_any;
 
-__device__ __forceinline__ float bf16_value(uint32_t h) { return __uint_as_float(h << 16); }
-__device__ __forceinline__ float f16_value(uint32_t h) {
-  return float(__builtin_bit_cast(_Float16, uint16_t(h)));
-}
-
 struct Four {
   float v[4];
 };
 
-// The first m (1 to 4) of four elements, zeros for the others.
-template <class T>
-__device__ __forceinline__ Four load_four(int dtype, const T *p, uint32_t m) {
-  Four r;
-  if (dtype == CHEB_F32) {
-    const float *f = reinterpret_cast<const float *>(p);
-    if (m == 4) {
-      const u32x4 t = *reinterpret_cast<const float4_any *>(f);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) r.v[i] = __uint_as_float(t[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) r.v[i] = uint32_t(i) < m ? f[i] : 0.0f;
-    }
-    return r;
-  }
-  const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
-  uint32_t t[4];
-  if (m == 4) {
-    const u32x2 u = *reinterpret_cast<const half4_any *>(h);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) t[i] = u[i >> 1] >> (16 * (i & 1)) & 0xffffu;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) t[i] = uint32_t(i) < m ? h[i] : 0u;
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) r.v[i] = dtype == CHEB_BF16 ? bf16_value(t[i]) : f16_value(t[i]);
-  return r;
-}
-
-__device__ __forceinline__ void store_four(int dtype, void *base, uint64_t at, const Four &x,
-                                           uint32_t m) {
-  if (dtype == CHEB_F32) {
-    float *f = static_cast<float *>(base) + at;
-    if (m == 4) {
-      u32x4 t;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) t[i] = __float_as_uint(x.v[i]);
-      *reinterpret_cast<float4_any *>(f) = t;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (uint32_t(i) < m) f[i] = x.v[i];
-    }
-    return;
-  }
-  uint16_t *h = static_cast<uint16_t *>(base) + at;
-  uint32_t t[2];
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const f32x2 p = {x.v[2 * q], x.v[2 * q + 1]};
-    t[q] = dtype == CHEB_BF16
-               ? __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2))
-               : __builtin_bit_cast(uint32_t, __builtin_convertvector(p, f16x2));
-  }
-  if (m == 4) {
-    *reinterpret_cast<half4_any *>(h) = u32x2{t[0], t[1]};
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (uint32_t(i) < m) h[i] = uint16_t(t[i >> 1] >> (16 * (i & 1)));
-  }
-}
-
-// Sources of a storage type: element e at base + e, or in 32 KiB chunks.
-template <int DT>
-struct PlainSrc {
-  static constexpr uint32_t kSize = DT == CHEB_F32 ? 4 : 2;
-  static constexpr int kLg = DT == CHEB_F32 ? 13 : 14;  // elements of a chunk
-  __device__ __forceinline__ static Four load(const NormArgs &a, int k, uint64_t e, uint32_t m) {
-    const char *b = reinterpret_cast<const char *>(a.base[k]);
-    if (!a.chunked) return load_four(DT, b + e * kSize, m);
-    const uint32_t in = uint32_t(e) & ((1u << kLg) - 1u);
-    const char *p = b + (e >> kLg) * a.super + in * kSize;
-    if (in + m <= 1u << kLg) return load_four(DT, p, m);
-    // across a chunk's end, element by element
-    Four r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint64_t f = e + uint64_t(i);
-      const char *q = b + (f >> kLg) * a.super + (uint32_t(f) & ((1u << kLg) - 1u)) * kSize;
-      r.v[i] = uint32_t(i) < m ? load_four(DT, q, 1).v[0] : 0.0f;
-    }
-    return r;
-  }
+// Four stored elements as loaded, converted later, so that loads follow one
+// another without a wait.
+struct Raw {
+  uint32_t u[4];
 };
 
-// 8-bit entries.
-template <class Fmt>
-struct CodedSrc {
-  __device__ __forceinline__ static float scale(const NormArgs &a, int k, uint64_t e) {
-    const uint32_t r = uint32_t(e) & uint32_t(kCodedChunk - 1);
-    const uint8_t *s = reinterpret_cast<const uint8_t *>(a.scales[k]) +
-                       (e >> kCodedChunkLg) * a.scale_super + (r >> 12) * 128u +
-                       (r >> 5 & 15u) * 8u + (r >> 9 & 7u);
-    return __uint_as_float(uint32_t(*s) << 23);
+__device__ __forceinline__ Raw raw_of(u32x4 t) { return {{t[0], t[1], t[2], t[3]}}; }
+__device__ __forceinline__ Raw raw_of(u32x2 t) { return {{t[0], t[1], 0u, 0u}}; }
+
+template <int DT>
+struct Stored {
+  static constexpr uint32_t kSize = DT == CHEB_F32 ? 4 : 2;
+
+  __device__ __forceinline__ static Raw four(const char *p) {
+    if constexpr (DT == CHEB_F32) return raw_of(*reinterpret_cast<const float4_any *>(p));
+    else return raw_of(*reinterpret_cast<const half4_any *>(p));
   }
-  __device__ __forceinline__ static const uint8_t *code(const NormArgs &a, int k, uint64_t e) {
-    return reinterpret_cast<const uint8_t *>(a.base[k]) + (e >> kCodedChunkLg) * a.super +
-           (uint32_t(e) & uint32_t(kCodedChunk - 1));
+  // Element q of the four.
+  __device__ __forceinline__ static void one(Raw &r, int q, const char *p) {
+    if constexpr (DT == CHEB_F32) r.u[q] = *reinterpret_cast<const uint32_t *>(p);
+    else r.u[q >> 1] |= uint32_t(*reinterpret_cast<const uint16_t *>(p)) << (16 * (q & 1));
   }
-  __device__ __forceinline__ static Four load(const NormArgs &a, int k, uint64_t e, uint32_t m) {
-    Four r;
-    float q[8];
-    if (m == 4 && (uint32_t(e) & 31u) <= 28u) {
-      Fmt::decode(u32x2{*reinterpret_cast<const code4_any *>(code(a, k, e)), 0u}, q);
-      const float s = scale(a, k, e) * float(Fmt::kUnit);
+  __device__ __forceinline__ static Four values(const Raw &r) {
+    Four x;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) r.v[i] = q[i] * s;
-      return r;
-    }
-    // across a group's end, or a row's, element by element
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      r.v[i] = 0.0f;
-      if (uint32_t(i) < m) {
-        Fmt::decode(u32x2{*code(a, k, e + uint64_t(i)), 0u}, q);
-        r.v[i] = q[0] * (scale(a, k, e + uint64_t(i)) * float(Fmt::kUnit));
+    for (int q = 0; q < 4; ++q) {
+      if constexpr (DT == CHEB_F32) {
+        x.v[q] = __uint_as_float(r.u[q]);
+      } else {
+        const uint32_t h = r.u[q >> 1] >> (16 * (q & 1));
+        x.v[q] = DT == CHEB_BF16 ? __uint_as_float(h << 16)
+                                 : float(__builtin_bit_cast(_Float16, uint16_t(h)));
       }
     }
-    return r;
+    return x;
   }
 };
 
-// Sums and maxima over the L threads of a row; every one gets the result.
-template <int L>
-struct RowOf {
-  static constexpr int kWaves = L > 64 ? L / 64 : 1;
+// Which elements of a lane's four are the row's own: those from lo up to hi
+// (none: hi is 0).
+struct Own {
+  uint32_t lo, hi;
+  __device__ __forceinline__ bool has(uint32_t q) const { return q >= lo && q < hi; }
+  __device__ __forceinline__ bool all() const { return lo == 0 && hi == 4; }
+};
 
-  __device__ __forceinline__ static double sum(double v, double *shared) {
+template <int DT>
+__device__ __forceinline__ void store_four(char *p, const Four &x, const Own &own) {
+  if constexpr (DT == CHEB_F32) {
+    if (own.all()) {
+      u32x4 t;
 #pragma unroll
-    for (int o = 1; o < (L < 64 ? L : 64); o *= 2) v += __shfl_xor(v, o);
-    if constexpr (kWaves > 1) {
-      if ((threadIdx.x & 63u) == 0) shared[threadIdx.x >> 6] = v;
-      __syncthreads();
-      v = 0.0;
+      for (int q = 0; q < 4; ++q) t[q] = __float_as_uint(x.v[q]);
+      *reinterpret_cast<float4_any *>(p) = t;
+    } else {
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) v += shared[w];
+      for (int q = 0; q < 4; ++q)
+        if (own.has(uint32_t(q))) reinterpret_cast<float *>(p)[q] = x.v[q];
     }
-    return v;
+  } else {
+    uint32_t t[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f32x2 v = {x.v[2 * h], x.v[2 * h + 1]};
+      if constexpr (DT == CHEB_BF16)
+        t[h] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+      else
+        t[h] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+    }
+    if (own.all()) {
+      *reinterpret_cast<half4_any *>(p) = u32x2{t[0], t[1]};
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (own.has(uint32_t(q)))
+          reinterpret_cast<uint16_t *>(p)[q] = uint16_t(t[q >> 1] >> (16 * (q & 1)));
+    }
   }
+}
 
-  __device__ __forceinline__ static uint32_t top(uint32_t v, uint32_t *shared) {
+// Where a row of the sources starts: `rb` bytes (scales: `rs`) from an entry's
+// base, `in` elements into a chunk (0: contiguous sources).
+struct RowAt {
+  uint64_t rb, rs;
+  uint32_t in;
+};
+
+// Sources of a storage type: contiguous, or in 32 KiB chunks.
+template <int DT>
+struct PlainSrc {
+  using Type = Stored<DT>;
+  using Held = Raw;
+  using At = uint32_t;                                      // bytes from the row's base
+  static constexpr uint32_t kLg = DT == CHEB_F32 ? 13 : 14;  // elements of a chunk
+  static constexpr bool kAnyPlace = true;                    // fours may start at any element
+
+  __device__ __forceinline__ static RowAt row(const NormArgs &a, uint64_t e) {
+    if (!a.chunked) return {e * Type::kSize, 0u, 0u};
+    return {(e >> kLg) * a.super, 0u, uint32_t(e) & ((1u << kLg) - 1u)};
+  }
+  __device__ __forceinline__ static At at(const NormArgs &a, const RowAt &r, uint32_t el) {
+    if (!a.chunked) return el * Type::kSize;
+    const uint32_t in = r.in + el;
+    return (in >> kLg) * a.super + (in & ((1u << kLg) - 1u)) * Type::kSize;
+  }
+  __device__ __forceinline__ static Held four(const NormArgs &a, int k, const RowAt &r, At at) {
+    return Type::four(reinterpret_cast<const char *>(a.base[k] + r.rb) + at);
+  }
+  __device__ __forceinline__ static Held some(const NormArgs &a, int k, const RowAt &r,
+                                              uint32_t el, const Own &own) {
+    Held h = {{0u, 0u, 0u, 0u}};
 #pragma unroll
-    for (int o = 1; o < (L < 64 ? L : 64); o *= 2) v = max(v, uint32_t(__shfl_xor(int(v), o)));
-    if constexpr (kWaves > 1) {
-      if ((threadIdx.x & 63u) == 0) shared[threadIdx.x >> 6] = v;
-      __syncthreads();
-      v = 0u;
+    for (int q = 0; q < 4; ++q)
+      if (own.has(uint32_t(q)))
+        Type::one(h, q, reinterpret_cast<const char *>(a.base[k] + r.rb) +
+                            at(a, r, el + uint32_t(q)));
+    return h;
+  }
+  __device__ __forceinline__ static Four values(const Held &h) { return Type::values(h); }
+};
+
+// 8-bit entries: four codes and, a byte each, their scales.
+template <class Fmt>
+struct CodedSrc {
+  struct Held {
+    uint32_t codes, scales;
+  };
+  struct At {
+    uint32_t code, scale;
+  };
+  static constexpr bool kAnyPlace = false;
+
+  __device__ __forceinline__ static RowAt row(const NormArgs &a, uint64_t e) {
+    return {(e >> kCodedChunkLg) * a.super, (e >> kCodedChunkLg) * a.scale_super,
+            uint32_t(e) & uint32_t(kCodedChunk - 1)};
+  }
+  __device__ __forceinline__ static At at(const NormArgs &a, const RowAt &r, uint32_t el) {
+    const uint32_t in = r.in + el, chunk = in >> kCodedChunkLg;
+    const uint32_t e = in & uint32_t(kCodedChunk - 1);
+    return {chunk * a.super + e,
+            chunk * a.scale_super + (e >> 12) * 128u + (e >> 5 & 15u) * 8u + (e >> 9 & 7u)};
+  }
+  __device__ __forceinline__ static Held four(const NormArgs &a, int k, const RowAt &r, At at) {
+    return {*reinterpret_cast<const code4_any *>(a.base[k] + r.rb + at.code),
+            uint32_t(*reinterpret_cast<const uint8_t *>(a.scales[k] + r.rs + at.scale)) *
+                0x01010101u};
+  }
+  __device__ __forceinline__ static Held some(const NormArgs &a, int k, const RowAt &r,
+                                              uint32_t el, const Own &own) {
+    Held h = {0u, 0u};
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) v = max(v, shared[w]);
-    }
-    return v;
+    for (int q = 0; q < 4; ++q)
+      if (own.has(uint32_t(q))) {
+        const At p = at(a, r, el + uint32_t(q));
+        h.codes |= uint32_t(*reinterpret_cast<const uint8_t *>(a.base[k] + r.rb + p.code))
+                   << (8 * q);
+        h.scales |= uint32_t(*reinterpret_cast<const uint8_t *>(a.scales[k] + r.rs + p.scale))
+                    << (8 * q);
+      }
+    return h;
+  }
+  __device__ __forceinline__ static Four values(const Held &h) {
+    float c[8];
+    Fmt::decode(u32x2{h.codes, 0u}, c);
+    Four x;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      x.v[q] = c[q] * (__uint_as_float((h.scales >> (8 * q) & 255u) << 23) * float(Fmt::kUnit));
+    return x;
   }
 };
 
-__device__ __forceinline__ uint32_t magnitude_of(const Four &y) {
-  uint32_t t = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) t = max(t, __float_as_uint(y.v[i]) & 0x7fffffffu);
-  return t;
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved(uint32_t v) {
+  return uint32_t(__builtin_amdgcn_mov_dpp(int(v), CTRL, 0xF, 0xF, true));
+}
+template <int CTRL>
+__device__ __forceinline__ double moved(double v) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, uint64_t(moved<CTRL>(uint32_t(b))) |
+                                        uint64_t(moved<CTRL>(uint32_t(b >> 32))) << 32);
+}
+
+// Joins the values of the L (up to 64) neighbouring lanes of a row: exchanges
+// within fours, eights and sixteens by mirrors (both halves hold one value each
+// by then), then across.
+template <int L, class T, class Join>
+__device__ __forceinline__ T join_lanes(T v, Join join) {
+  v = join(v, moved<0xB1>(v));   // 1 0 3 2
+  v = join(v, moved<0x4E>(v));   // 2 3 0 1
+  v = join(v, moved<0x141>(v));  // mirrored in eights
+  if constexpr (L >= 16) v = join(v, moved<0x140>(v));  // in sixteens
+  if constexpr (L >= 32) v = join(v, __shfl_xor(v, 16));
+  if constexpr (L >= 64) v = join(v, __shfl_xor(v, 32));
+  return v;
 }
 
 // Codes of y times `factor` (0: codes 0, whatever y holds).
-__device__ __forceinline__ void store_codes(void *base, uint64_t at, const Four &y, float factor,
-                                            uint32_t m) {
+__device__ __forceinline__ void store_codes(char *p, const Four &y, float factor,
+                                            const Own &own) {
   float v[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = factor == 0.0f ? 0.0f : y.v[i] * factor;
-  int p = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
-  p = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], p, true);
-  uint8_t *b = static_cast<uint8_t *>(base) + at;
-  if (m == 4) {
-    *reinterpret_cast<code4_any *>(b) = uint32_t(p);
+  for (int q = 0; q < 4; ++q) v[q] = factor == 0.0f ? 0.0f : y.v[q] * factor;
+  int c = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
+  c = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], c, true);
+  if (own.all()) {
+    *reinterpret_cast<code4_any *>(p) = uint32_t(c);
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (uint32_t(i) < m) b[i] = uint8_t(p >> (8 * i));
+    for (int q = 0; q < 4; ++q)
+      if (own.has(uint32_t(q))) reinterpret_cast<uint8_t *>(p)[q] = uint8_t(c >> (8 * q));
   }
 }
 
-// L threads hold a row, P times four elements each: thread t's i-th four are
-// elements (i L + t) * 4 on.
-template <class Src, int L, int P>
+// How a row's elements fall into fours.
+//   kEven  dim is a multiple of four (and so is the sources' first element,
+//          where fours must not cross a chunk or a group): every four is the
+//          row's own or none of it is.
+//   kOdd   contiguous sources of any dim: a row's last four reaches into the next
+//          row, and in the last rows, which have none, starts earlier instead.
+//   kSplit sources whose fours may cross a chunk or a group, or of fewer than
+//          four elements in all: element by element.
+enum { kEven, kOdd, kSplit };
+
+template <int DT, int L, int P, int M>
+__device__ __forceinline__ void load_x(Raw (&x)[P], const char *p, const uint32_t (&el)[P],
+                                       const Own (&own)[P]) {
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    if constexpr (M != kSplit) {
+      x[i] = Stored<DT>::four(p + int64_t(int32_t(el[i])) * Stored<DT>::kSize);
+    } else {
+      x[i] = Raw{{0u, 0u, 0u, 0u}};
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (own[i].has(uint32_t(q)))
+          Stored<DT>::one(x[i], q, p + (el[i] + uint32_t(q)) * Stored<DT>::kSize);
+    }
+  }
+}
+
+template <int DT, int P>
+__device__ __forceinline__ void store_rows(void *to, uint64_t r0, const Four (&x)[P],
+                                           const uint32_t (&el)[P], const Own (&own)[P]) {
+  char *p = static_cast<char *>(to) + r0 * Stored<DT>::kSize;
+#pragma unroll
+  for (int i = 0; i < P; ++i)
+    if (own[i].hi)
+      store_four<DT>(p + int64_t(int32_t(el[i])) * Stored<DT>::kSize, x[i], own[i]);
+}
+
+// L threads hold a row, P times four elements each: thread t's i-th four is
+// elements (i L + t) * 4 on.  B sources are loaded ahead of their sums.
+template <class Src, int L, int P, int B, int M>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a) {
-  constexpr int kThreads = L < 256 ? 256 : L;
-  __shared__ double sums[2][16];
-  __shared__ uint32_t tops[16];
+  constexpr int kThreads = L < 256 ? 256 : L, kWaves = L > 64 ? L / 64 : 1;
+  __shared__ double sums[kWaves][3];
+  __shared__ uint32_t tops[kWaves];
   const uint32_t t = threadIdx.x % uint32_t(L);
-  const uint32_t row = blockIdx.x * uint32_t(kThreads / L) + threadIdx.x / uint32_t(L);
+  uint32_t row = blockIdx.x * uint32_t(kThreads / L) + threadIdx.x / uint32_t(L);
+  if constexpr (L >= 64) row = __builtin_amdgcn_readfirstlane(row);
   if (row >= a.rows) return;  // a whole row's threads; only L < 256, which meets no barrier
   const uint64_t r0 = uint64_t(row) * a.dim;
-  uint32_t m[P];  // elements of each four within the row
+  uint32_t el[P];  // first element of each four (kOdd: may lie before the row)
+  Own own[P];
 #pragma unroll
   for (int i = 0; i < P; ++i) {
     const uint32_t e = (uint32_t(i) * L + t) * 4u;
-    m[i] = e < a.dim ? (a.dim - e < 4u ? a.dim - e : 4u) : 0u;
+    own[i] = {0u, e < a.dim ? (M == kEven || a.dim - e >= 4u ? 4u : a.dim - e) : 0u};
+    el[i] = own[i].hi ? e : 0u;
+    if constexpr (M == kOdd) {
+      // elements from the row's first to the last row's last
+      const uint64_t left = uint64_t(a.rows - row) * a.dim;
+      if (uint64_t(el[i]) + 4u > left) {
+        const uint32_t by = el[i] + 4u - uint32_t(left);
+        el[i] -= by;
+        own[i].lo = own[i].hi ? by : 0u;
+        own[i].hi = own[i].hi ? own[i].hi + by : 0u;
+      }
+    }
+  }
+  const RowAt from = Src::row(a, a.first + r0);
+  typename Src::At at[P];
+  if constexpr (M == kEven) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) at[i] = Src::at(a, from, el[i]);
   }
   double acc[P][4];
 #pragma unroll
   for (int i = 0; i < P; ++i)
 #pragma unroll
     for (int q = 0; q < 4; ++q) acc[i][q] = -0.0;  // the sum of nothing: x + -0.0 is x, -0.0 too
-  Four x[P], s[P];
+  Raw x0[P];
 #pragma unroll
-  for (int i = 0; i < P; ++i) {
-    x[i] = Four{{0.0f, 0.0f, 0.0f, 0.0f}};
-    const uint64_t e = r0 + (uint32_t(i) * L + t) * 4u;
-    if (a.x_in && m[i])
-      x[i] = load_four(a.x_dtype,
-                       static_cast<const char *>(a.x_in) + e * (a.x_dtype == CHEB_F32 ? 4u : 2u),
-                       m[i]);
+  for (int i = 0; i < P; ++i) x0[i] = Raw{{0u, 0u, 0u, 0u}};
+  if (a.x_in) {
+    const char *p = static_cast<const char *>(a.x_in);
+    if (a.x_dtype == CHEB_F32) load_x<CHEB_F32, L, P, M>(x0, p + r0 * 4u, el, own);
+    else load_x<CHEB_BF16, L, P, M>(x0, p + r0 * 2u, el, own);
   }
-  for (int k = 0; k < a.n; ++k) {
+  for (int k = 0; k < a.n; k += B) {
+    typename Src::Held s[B][P];
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-      s[i] = Four{{0.0f, 0.0f, 0.0f, 0.0f}};
-      if (m[i]) s[i] = Src::load(a, k, a.first + r0 + (uint32_t(i) * L + t) * 4u, m[i]);
-    }
-    const double w = a.w[k];
+    for (int j = 0; j < B; ++j)
+      if (k + j < a.n) {
 #pragma unroll
-    for (int i = 0; i < P; ++i)
+        for (int i = 0; i < P; ++i) {
+          if constexpr (M == kEven) {
+            s[j][i] = Src::four(a, k + j, from, at[i]);
+          } else if constexpr (M == kOdd) {
+            if constexpr (Src::kAnyPlace)
+              s[j][i] = Src::Type::four(reinterpret_cast<const char *>(a.base[k + j] + from.rb) +
+                                        int64_t(int32_t(el[i])) * Src::Type::kSize);
+          } else {
+            uint32_t e = el[i];
+            asm volatile("" : "+v"(e));  // places formed anew for each source, not kept for all
+            s[j][i] = Src::some(a, k + j, from, e, own[i]);
+          }
+        }
+      }
 #pragma unroll
-      for (int q = 0; q < 4; ++q) acc[i][q] = fma(w, double(s[i].v[q]), acc[i][q]);
-  }
-  double sum = 0.0, squares = 0.0;
+    for (int j = 0; j < B; ++j)
+      if (k + j < a.n) {
+        const double w = a.w[k + j];
 #pragma unroll
-  for (int i = 0; i < P; ++i) {
+        for (int i = 0; i < P; ++i) {
+          const Four v = Src::values(s[j][i]);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      x[i].v[q] = float(double(x[i].v[q]) + acc[i][q]);
-      if (uint32_t(q) >= m[i]) x[i].v[q] = 0.0f;
-      sum += double(x[i].v[q]);
-      squares = fma(double(x[i].v[q]), double(x[i].v[q]), squares);
-    }
-    if (a.x_out && m[i])
-      store_four(a.x_dtype, a.x_out, r0 + (uint32_t(i) * L + t) * 4u, x[i], m[i]);
-  }
-  if (a.layer) {
-    const double mean = RowOf<L>::sum(sum, sums[0]) * a.inv_dim;
-    squares = 0.0;
-#pragma unroll
-    for (int i = 0; i < P; ++i)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        x[i].v[q] = uint32_t(q) < m[i] ? float(double(x[i].v[q]) - mean) : 0.0f;
-        squares = fma(double(x[i].v[q]), double(x[i].v[q]), squares);
+          for (int q = 0; q < 4; ++q) acc[i][q] = fma(w, double(v.v[q]), acc[i][q]);
+        }
       }
   }
-  const float r =
-      float(1.0 / sqrt(RowOf<L>::sum(squares, sums[1]) * a.inv_dim + a.eps));
-  const uint64_t g0 = a.gain || a.shift ? uint64_t(row / a.rows_per_group) * a.dim : 0u;
-  uint32_t top = 0;
+  Four x[P];
 #pragma unroll
-  for (int i = 0; i < P; ++i) {
-    const uint32_t e = (uint32_t(i) * L + t) * 4u;
-    Four g = {{1.0f, 1.0f, 1.0f, 1.0f}}, b = {{0.0f, 0.0f, 0.0f, 0.0f}};
-    if (a.gain && m[i]) g = load_four(CHEB_F32, a.gain + g0 + e, m[i]);
-    if (a.shift && m[i]) b = load_four(CHEB_F32, a.shift + g0 + e, m[i]);
+  for (int i = 0; i < P; ++i)
+    x[i] = a.x_dtype == CHEB_F32    ? Stored<CHEB_F32>::values(x0[i])
+           : a.x_dtype == CHEB_BF16 ? Stored<CHEB_BF16>::values(x0[i])
+                                    : Stored<CHEB_F16>::values(x0[i]);
+#pragma unroll
+  for (int i = 0; i < P; ++i)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) x[i].v[q] = float(double(x[i].v[q]) + acc[i][q]);
+  if (a.x_out) {
+    if (a.x_dtype == CHEB_F32) store_rows<CHEB_F32, P>(a.x_out, r0, x, el, own);
+    else if (a.x_dtype == CHEB_BF16) store_rows<CHEB_BF16, P>(a.x_out, r0, x, el, own);
+    else store_rows<CHEB_F16, P>(a.x_out, r0, x, el, own);
+  }
+  // Sums about the row's first element, so that one pass gives the mean and
+  // the squares about it: x - x_0 loses nothing in fp64 that matters to x.
+  double about = 0.0, sum = 0.0, squares = 0.0;
+  if (a.layer) {
+    float f = 0.0f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (uint32_t(q) == own[0].lo) f = x[0].v[q];
+    about = double(__shfl(f, 0, L < 64 ? L : 64));
+    if constexpr (kWaves > 1) {
+      if (threadIdx.x == 0) sums[0][2] = about;
+      __syncthreads();
+      about = sums[0][2];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < P; ++i)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const float y = x[i].v[q] * r;
-      x[i].v[q] = a.gain ? y * g.v[q] : y;
-      if (a.shift) x[i].v[q] += b.v[q];
-      if (uint32_t(q) >= m[i]) x[i].v[q] = 0.0f;
+      const double d = own[i].has(uint32_t(q)) ? double(x[i].v[q]) - about : 0.0;
+      sum += d;
+      squares = fma(d, d, squares);
     }
-    top = max(top, magnitude_of(x[i]));
+  const auto add = [](double u, double v) { return u + v; };
+  constexpr int kLanes = L < 64 ? L : 64;
+  squares = join_lanes<kLanes>(squares, add);
+  if (a.layer) sum = join_lanes<kLanes>(sum, add);
+  if constexpr (kWaves > 1) {
+    if ((threadIdx.x & 63u) == 0) {
+      sums[threadIdx.x >> 6][0] = sum;
+      sums[threadIdx.x >> 6][1] = squares;
+    }
+    __syncthreads();
+    sum = squares = 0.0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      sum += sums[w][0];
+      squares += sums[w][1];
+    }
   }
+  double mean = 0.0, var = squares * a.inv_dim;
+  if (a.layer) {
+    const double off = sum * a.inv_dim;
+    mean = about + off;
+    var = fma(-off, off, var);
+    if (var < 0.0) var = 0.0;  // by rounding; a NaN stays
+  }
+  const float r = float(1.0 / sqrt(var + a.eps));
+#pragma unroll
+  for (int i = 0; i < P; ++i)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      x[i].v[q] = (a.layer ? float(double(x[i].v[q]) - mean) : x[i].v[q]) * r;
+  if (a.gain || a.shift) {
+    const uint64_t g0 = uint64_t(row / a.rows_per_group) * a.dim;
+    const auto row_of = [&](const float *p, Four (&g)[P]) {
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const float *e = p + g0 + int64_t(int32_t(el[i]));
+        if constexpr (M == kEven) {
+          g[i] = Stored<CHEB_F32>::values(
+              Stored<CHEB_F32>::four(reinterpret_cast<const char *>(e)));
+        } else {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) g[i].v[q] = own[i].has(uint32_t(q)) ? e[q] : 0.0f;
+        }
+      }
+    };
+    if (a.gain) {
+      Four g[P];
+      row_of(a.gain, g);
+#pragma unroll
+      for (int i = 0; i < P; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[i].v[q] *= g[i].v[q];
+    }
+    if (a.shift) {
+      Four g[P];
+      row_of(a.shift, g);
+#pragma unroll
+      for (int i = 0; i < P; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[i].v[q] += g[i].v[q];
+    }
+  }
+  const auto highest = [](uint32_t u, uint32_t v) { return max(u, v); };
+  const auto magnitude = [&](int i) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (own[i].has(uint32_t(q))) m = max(m, __float_as_uint(x[i].v[q]) & 0x7fffffffu);
+    return m;
+  };
+  char *codes = static_cast<char *>(a.y) + r0;
   if (a.out_format == CHEB_OUT_MXFP8) {
     const uint32_t width = (a.dim + 31u) / 32u;
+    uint8_t *scales = static_cast<uint8_t *>(a.y_scale) + uint64_t(row) * width;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      // the eight threads of a group: two exchanges in fours, then the fours
-      uint32_t g = quad_max(magnitude_of(x[i]));
-      g = max(g, uint32_t(__builtin_amdgcn_mov_dpp(int(g), 0x141, 0xF, 0xF, true)));
-      const Group of = group_of<E4m3Fmt>(g);
-      const uint32_t e = (uint32_t(i) * L + t) * 4u;
-      if (m[i]) store_codes(a.y, r0 + e, x[i], of.factor, m[i]);
-      if (m[i] && (t & 7u) == 0)
-        static_cast<uint8_t *>(a.y_scale)[uint64_t(row) * width + e / 32u] = uint8_t(of.scale);
+      const Group of = group_of<E4m3Fmt>(join_lanes<8>(magnitude(i), highest));
+      if (own[i].hi) {
+        store_codes(codes + int64_t(int32_t(el[i])), x[i], of.factor, own[i]);
+        if ((t & 7u) == 0) scales[(uint32_t(i) * L + t) / 8u] = uint8_t(of.scale);
+      }
     }
-    return;
-  }
-  if (a.out_format == CHEB_OUT_FP8_ROW) {
-    const uint32_t bits = RowOf<L>::top(top, tops);
+  } else if (a.out_format == CHEB_OUT_FP8_ROW) {
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < P; ++i) bits = max(bits, magnitude(i));
+    bits = join_lanes<kLanes>(bits, highest);
+    if constexpr (kWaves > 1) {
+      if ((threadIdx.x & 63u) == 0) tops[threadIdx.x >> 6] = bits;
+      __syncthreads();
+      bits = 0u;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) bits = max(bits, tops[w]);
+    }
     float scale = 1.0f, factor = 1.0f;
     if (bits >= 0x7f800000u) {
       scale = __uint_as_float(0x7fc00000u);
@@ -342,19 +515,29 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a) {
     if (t == 0) static_cast<float *>(a.y_scale)[row] = scale;
 #pragma unroll
     for (int i = 0; i < P; ++i)
-      if (m[i]) store_codes(a.y, r0 + (uint32_t(i) * L + t) * 4u, x[i], factor, m[i]);
-    return;
+      if (own[i].hi) store_codes(codes + int64_t(int32_t(el[i])), x[i], factor, own[i]);
+  } else if (a.out_format == CHEB_F32) {
+    store_rows<CHEB_F32, P>(a.y, r0, x, el, own);
+  } else if (a.out_format == CHEB_BF16) {
+    store_rows<CHEB_BF16, P>(a.y, r0, x, el, own);
+  } else {
+    store_rows<CHEB_F16, P>(a.y, r0, x, el, own);
   }
-#pragma unroll
-  for (int i = 0; i < P; ++i)
-    if (m[i]) store_four(a.out_format, a.y, r0 + (uint32_t(i) * L + t) * 4u, x[i], m[i]);
 }
 
 template <class Src, int L, int P>
 hipError_t launch_shape(const NormArgs &a, hipStream_t s) {
   constexpr uint32_t kThreads = L < 256 ? 256 : L, kRows = kThreads / L;
-  hipLaunchKernelGGL((norm_kernel<Src, L, P>), dim3((a.rows + kRows - 1) / kRows), dim3(kThreads),
-                     0, s, a);
+  constexpr int B = P <= 2 ? 4 : 2;
+  const bool placed = a.chunked || !Src::kAnyPlace;  // fours must not cross
+  const bool even = a.dim % 4u == 0 && (!placed || a.first % 4u == 0);
+  auto kernel = norm_kernel<Src, L, P, B, kEven>;
+  if (!even) {
+    kernel = norm_kernel<Src, L, P, 1, kSplit>;
+    if constexpr (Src::kAnyPlace)
+      if (!placed && uint64_t(a.rows) * a.dim >= 4u) kernel = norm_kernel<Src, L, P, B, kOdd>;
+  }
+  hipLaunchKernelGGL(kernel, dim3((a.rows + kRows - 1) / kRows), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 
@@ -401,7 +584,7 @@ int launch_norm(const NormSources &from, const cheb_norm &n, hipStream_t stream)
   a.first = uint64_t(from.first);
   a.n = from.n;
   a.chunked = from.super_vecs != kChunkVecs;
-  a.super = uint64_t(from.super_vecs) * 16u;
+  a.super = uint32_t(from.super_vecs) * 16u;
   a.x_in = n.x_in;
   a.x_out = n.x_out;
   a.gain = n.gain;
@@ -418,8 +601,8 @@ int launch_norm(const NormSources &from, const cheb_norm &n, hipStream_t stream)
   a.out_format = n.out_format;
   hipError_t e;
   if (from.quant != CHEB_QUANT_NONE) {
-    a.super = from.place.code_super;
-    a.scale_super = from.place.scale_super;
+    a.super = uint32_t(from.place.code_super);
+    a.scale_super = uint32_t(from.place.scale_super);
     e = from.quant == CHEB_QUANT_MXINT8 ? launch_src<CodedSrc<Int8Fmt>>(a, stream)
                                         : launch_src<CodedSrc<E4m3Fmt>>(a, stream);
   } else if (from.dtype == CHEB_BF16) {
