@@ -52,10 +52,10 @@ def cheb_dtype(dtype: torch.dtype) -> int:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream_handle(stream: Optional[torch.cuda.Stream]) -> int:
+def _stream_handle(stream: Optional[torch.cuda.Stream], device: Optional[int] = None) -> int:
     if stream is None:
         if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
+            return _raw_stream(torch.cuda.current_device() if device is None else device)
         stream = torch.cuda.current_stream()
     return int(stream.cuda_stream)
 
@@ -216,63 +216,76 @@ def norm_output(rows: int, dim: int, out=torch.bfloat16, device=None):
     return y, torch.empty(rows, -(-dim // 32), dtype=torch.float8_e8m0fnu, device=device)
 
 
-def _norm_call(tensors, x_out, x_in, numel, dim, kind, eps, gain, shift, out):
-    """The norm's structure and its output's buffers; every tensor of the call
-    is checked, and lies on the current device."""
-    for t, what in ((x_out, "x_out"), (x_in, "x_in"), (gain, "gain"), (shift, "shift")):
-        if t is not None:
-            _check_device_tensor(t, what)
-    x = x_in if x_in is not None else x_out
-    if x_in is not None and x_out is not None and (x_in.dtype != x_out.dtype
-                                                   or x_in.numel() != x_out.numel()):
-        raise ChebError(_binding.CHEB_E_MISMATCH, "x_in differs from x_out")
-    if x is not None and x.numel() != numel:
-        raise ChebError(_binding.CHEB_E_MISMATCH, f"the residual holds {x.numel()} elements, "
-                        f"the sources {numel}")
-    dim = int(dim)
+def _here(t, what: str, current: int):
+    """Refuses what is no contiguous tensor of the current device."""
+    if isinstance(t, torch.Tensor) and t.get_device() == current and t.is_contiguous():
+        return
+    _check_device_tensor(t, what)
+    raise ChebError(_binding.CHEB_E_INVAL,
+                    f"{what} is on {t.device}, the current device is {current}")
+
+
+def _norm_rows(t, what: str, dim: int, rows: int) -> int:
+    """Groups of a gain or shift."""
+    n = t.numel()
+    if t.dtype is not torch.float32 or n == 0 or n % dim:
+        raise ChebError(_binding.CHEB_E_MISMATCH, f"{what} must be float32 rows of {dim}")
+    if rows % (n // dim):
+        raise ChebError(_binding.CHEB_E_MISMATCH, f"{what}: {rows} rows in {n // dim} groups")
+    return n // dim
+
+
+def _norm_call(current, device, x_out, x_in, numel, dim, kind, eps, gain, shift, out):
+    """The norm's structure and its output's buffers; every tensor it takes is
+    checked, and lies on the current device."""
+    x_dt = CHEB_F32
+    in_ptr = out_ptr = gain_ptr = shift_ptr = scale_ptr = None
+    if x_in is not None:
+        _here(x_in, "x_in", current)
+        in_ptr, x_dt = x_in.data_ptr(), cheb_dtype(x_in.dtype)
+        if x_in.numel() != numel:
+            raise ChebError(_binding.CHEB_E_MISMATCH,
+                            f"x_in holds {x_in.numel()} elements, the sources {numel}")
+    if x_out is not None:
+        _here(x_out, "x_out", current)
+        out_ptr, x_dt = x_out.data_ptr(), cheb_dtype(x_out.dtype)
+        if x_out.numel() != numel or (x_in is not None and x_in.dtype is not x_out.dtype):
+            raise ChebError(_binding.CHEB_E_MISMATCH, "x_out differs from x_in or the sources")
     if dim < 1 or numel % dim:
         raise ChebError(_binding.CHEB_E_MISMATCH, f"{numel} elements are no rows of {dim}")
-    if kind not in _NORMS:
+    rows, groups = numel // dim, 0
+    norm = _NORMS.get(kind)
+    if norm is None:
         raise ChebError(_binding.CHEB_E_INVAL, f"unknown norm {kind!r}")
-    rows = numel // dim
-    groups = 0
-    for t, what in ((gain, "gain"), (shift, "shift")):
-        if t is None:
-            continue
-        if t.dtype is not torch.float32 or t.numel() == 0 or t.numel() % dim:
-            raise ChebError(_binding.CHEB_E_MISMATCH, f"{what} must be float32 rows of {dim}")
-        if groups not in (0, t.numel() // dim) or rows % (t.numel() // dim):
-            raise ChebError(_binding.CHEB_E_MISMATCH, f"{what}: {rows} rows in "
-                            f"{t.numel() // dim} groups, or not as many as the gain's")
-        groups = t.numel() // dim
+    if gain is not None:
+        _here(gain, "gain", current)
+        gain_ptr, groups = gain.data_ptr(), _norm_rows(gain, "gain", dim, rows)
+    if shift is not None:
+        _here(shift, "shift", current)
+        shift_ptr, of_shift = shift.data_ptr(), _norm_rows(shift, "shift", dim, rows)
+        if gain is not None and of_shift != groups:
+            raise ChebError(_binding.CHEB_E_MISMATCH, "gain and shift differ in groups")
+        groups = of_shift
     if isinstance(out, (str, torch.dtype)):
-        device = tensors[0].device if tensors else x.device
         out = norm_output(rows, dim, out, device)
-    y, scale = out if isinstance(out, tuple) else (out, None)
-    _check_device_tensor(y, "out")
-    if scale is None:
-        fmt = cheb_dtype(y.dtype)
-    else:
-        _check_device_tensor(scale, "out's scales")
+    if isinstance(out, tuple):
+        y, scale = out
+        _here(scale, "out's scales", current)
+        scale_ptr = scale.data_ptr()
         fmt = CHEB_OUT_FP8_ROW if scale.dtype is torch.float32 else CHEB_OUT_MXFP8
         want = rows if fmt == CHEB_OUT_FP8_ROW else rows * -(-dim // 32)
         if (y.dtype is not torch.float8_e4m3fn or scale.numel() != want
                 or (fmt == CHEB_OUT_MXFP8 and scale.dtype is not torch.float8_e8m0fnu)):
             raise ChebError(_binding.CHEB_E_MISMATCH, "out differs from norm_output's")
+    else:
+        y = out
+        fmt = cheb_dtype(y.dtype)
+    _here(y, "out", current)
     if y.numel() != numel:
         raise ChebError(_binding.CHEB_E_MISMATCH, f"out holds {y.numel()} elements, not {numel}")
-    current = torch.cuda.current_device()
-    for t in (*tensors, x_out, x_in, gain, shift, y, scale):
-        if t is not None and t.device.index != current:
-            raise ChebError(_binding.CHEB_E_INVAL,
-                            f"a tensor is on {t.device}, the current device is {current}")
-    norm = cheb_norm(rows, dim, float(eps), None if x_in is None else x_in.data_ptr(),
-                     None if x_out is None else x_out.data_ptr(),
-                     None if gain is None else gain.data_ptr(),
-                     None if shift is None else shift.data_ptr(), rows // groups if groups else 0,
-                     y.data_ptr(), None if scale is None else scale.data_ptr(), _NORMS[kind],
-                     CHEB_F32 if x is None else cheb_dtype(x.dtype), fmt)
-    return norm, out
+    return cheb_norm(rows, dim, eps, in_ptr, out_ptr, gain_ptr, shift_ptr,
+                     rows // groups if groups else 0, y.data_ptr(), scale_ptr, norm, x_dt,
+                     fmt), out
 
 
 def add_norm(srcs: Sequence[torch.Tensor], w, x_out: Optional[torch.Tensor] = None,
@@ -288,17 +301,22 @@ def add_norm(srcs: Sequence[torch.Tensor], w, x_out: Optional[torch.Tensor] = No
     if len(srcs) == 0 and x_in is None:
         raise ChebError(_binding.CHEB_E_INVAL, "neither sources nor x_in")
     like = srcs[0] if len(srcs) else x_in
-    _check_device_tensor(like, "srcs[0]" if len(srcs) else "x_in")
+    if not isinstance(like, torch.Tensor) or not like.is_cuda:
+        _check_device_tensor(like, "srcs[0]" if len(srcs) else "x_in")
+    current = torch.cuda.current_device()
     dtype, numel = like.dtype, like.numel()
-    dt = cheb_dtype(dtype)
-    for i, s in enumerate(srcs):
-        if not _plain(s, dtype, numel):
-            _check_device_tensor(s, f"srcs[{i}]")
-            raise ChebError(_binding.CHEB_E_MISMATCH, f"srcs[{i}] differs in dtype or size")
+    ptrs = []
+    for s in srcs:
+        _here(s, "a source", current)
+        if s.dtype is not dtype or s.numel() != numel:
+            raise ChebError(_binding.CHEB_E_MISMATCH,
+                            f"srcs[{len(ptrs)}] differs in dtype or size")
+        ptrs.append(s.data_ptr())
     if dim is None:
         dim = like.shape[-1] if like.dim() else 1
-    norm, out = _norm_call(srcs, x_out, x_in, numel, dim, kind, eps, gain, shift, out)
-    cheb_add_norm([s.data_ptr() for s in srcs], w, dt, norm, _stream_handle(stream))
+    norm, out = _norm_call(current, like.device, x_out, x_in, numel, dim, kind, eps, gain, shift,
+                           out)
+    cheb_add_norm(ptrs, w, cheb_dtype(dtype), norm, _stream_handle(stream, current))
     return x_out, out
 
 
@@ -602,9 +620,11 @@ class ChebCache:
         if dim < 1 or first < 0 or left < 0 or (rows is not None and rows < 0):
             raise ChebError(_binding.CHEB_E_INVAL, f"no rows of {dim} from element {first} on")
         rows = left // dim if rows is None else int(rows)
-        norm, out = _norm_call((self.arena,), x_out, x_in, rows * dim, dim, kind, eps, gain, shift,
-                               out)
-        cheb_residual_norm(self._h, w, seg, first, norm, _stream_handle(stream))
+        current = torch.cuda.current_device()
+        _here(self.arena, "the cache", current)
+        norm, out = _norm_call(current, self.device, x_out, x_in, rows * dim, dim, kind, eps, gain,
+                               shift, out)
+        cheb_residual_norm(self._h, w, seg, first, norm, _stream_handle(stream, current))
         return x_out, out
 
     def extrapolate_at(self, target_t: float, out: Optional[torch.Tensor] = None,

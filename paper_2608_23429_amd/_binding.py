@@ -537,11 +537,12 @@ def cheb_residual_reduce(seg_ptrs, seg_numel, res_offset, dtype, x_in_ptr, x_out
 
 def cheb_add_norm(src_ptrs, w, dtype, norm, stream=0):
     """norm: a cheb_norm structure."""
-    w = _f64(w).reshape(-1)
-    if w.size != len(src_ptrs):
+    w = _f64(w)
+    n = len(src_ptrs)
+    if w.size != n:
         raise ChebError(CHEB_E_INVAL, "one weight per source")
-    _check(LIB.cheb_add_norm(_voidp_array(src_ptrs), w.size, _dptr(w) if w.size else None,
-                             int(dtype), ctypes.byref(norm), int(stream)))
+    _check(LIB.cheb_add_norm(_voidp_array(src_ptrs), n, _dptr(w) if n else None, dtype,
+                             ctypes.byref(norm), stream))
 
 
 def cheb_residual_norm(handle, w, seg, first, norm, stream=0):

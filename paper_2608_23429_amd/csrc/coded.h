@@ -16,6 +16,16 @@ typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
+// The tile of a block where N neighbouring tiles share a line of scales: they
+// go to one XCD, whose L2 then reads the line once (blocks are dealt to the
+// eight XCDs in turn; tiles past the last whole 8 N keep their order).
+template <uint32_t N>
+__device__ __forceinline__ uint32_t line_tile(uint32_t block, uint32_t blocks) {
+  if (N == 1 || block >= blocks / (8u * N) * (8u * N)) return block;
+  const uint32_t q = block >> 3;
+  return (q / N * 8u + (block & 7u)) * N + q % N;
+}
+
 // A group's scale byte (2^(scale - 127), 255: NaN) and the factor that takes
 // values to codes (0 for a group that is not finite: its codes are 0, and 0
 // times the scale's infinity, 255 << 23, is NaN).
@@ -50,27 +60,37 @@ __device__ __forceinline__ Group group_of(uint32_t a) {
   return g;
 }
 
-// Eight codes of a lane.
+// A lane's eight codes.  decode() gives halves, pairs of exact fp16 numbers,
+// which v_fma_mix_f32 takes as they are; a code counts kUnit of its scale times
+// its half.  The conversions from integers and fp8 run at a quarter of the rate
+// of other instructions and would bound the sums over several entries; these
+// take full-rate ones.
+struct Halves {
+  f16x2 h[4];
+  __device__ __forceinline__ float operator[](int i) const { return float(h[i >> 1][i & 1]); }
+};
+
 struct Int8Fmt {
   static constexpr uint32_t kLimitFraction = 0x7e0000u;  // 127/64 = 1.984375
   static constexpr int kLimitExponent = 0;
   static constexpr int kShift = 6;        // a code counts 64ths of the scale
   static constexpr double kUnit = 0x1p-6;
 
-  // Adding 1.5 2^23 rounds to the nearest whole number, ties to even, and
-  // leaves it as the low byte of the sum's bits (x factor is exact: a power
-  // of two).
+  // The stored byte is the code plus 128.  Adding 1.5 2^23 + 128 rounds to the
+  // nearest whole number, ties to even, and leaves it as the low byte of the
+  // sum's bits (x factor is exact: a power of two).
   __device__ __forceinline__ static u32x2 encode(const float (&x)[8], const Group &g) {
+    constexpr float kWhole = 0x1.8p23f + 128.0f;
     uint32_t t[8];
     if (__builtin_expect(__ballot(g.top) != 0ull, 0)) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float v = g.factor == 0.0f ? 0.0f : fminf(fmaxf(x[i] * g.factor, -127.0f), 127.0f);
-        t[i] = __float_as_uint(v + 0x1.8p23f);
+        t[i] = __float_as_uint(v + kWhole);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) t[i] = __float_as_uint(fmaf(x[i], g.factor, 0x1.8p23f));
+      for (int i = 0; i < 8; ++i) t[i] = __float_as_uint(fmaf(x[i], g.factor, kWhole));
     }
     u32x2 r;
 #pragma unroll
@@ -82,9 +102,16 @@ struct Int8Fmt {
     return r;
   }
 
-  __device__ __forceinline__ static void decode(u32x2 v, float (&q)[8]) {
+  // 0x64 above a byte b is the fp16 number 1024 + b.
+  __device__ __forceinline__ static Halves decode(u32x2 v) {
+    const f16x2 off = {_Float16(-1152.0f), _Float16(-1152.0f)};
+    Halves q;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = float(int32_t(v[i >> 2] << (24 - 8 * (i & 3))) >> 24);
+    for (int i = 0; i < 4; ++i)
+      q.h[i] = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, v[i >> 1],
+                                                               i & 1 ? 0x04030402u : 0x04010400u)) +
+               off;
+    return q;
   }
 };
 
@@ -92,7 +119,7 @@ struct E4m3Fmt {
   static constexpr uint32_t kLimitFraction = 0x600000u;  // 448 = 1.75 2^8
   static constexpr int kLimitExponent = 8;
   static constexpr int kShift = 0;
-  static constexpr double kUnit = 1.0;
+  static constexpr double kUnit = 0x1p8;
 
   __device__ __forceinline__ static u32x2 encode(const float (&x)[8], const Group &g) {
     float v[8];
@@ -113,16 +140,18 @@ struct E4m3Fmt {
     return r;
   }
 
-  __device__ __forceinline__ static void decode(u32x2 v, float (&q)[8]) {
+  // The code's exponent and fraction one place below a half's sign are the
+  // fp16 number of 2^-8 its value (exponents are biased by 7 and 15), fp16's
+  // small numbers being e4m3's.  Codes are never NaN.
+  __device__ __forceinline__ static Halves decode(u32x2 v) {
+    Halves q;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(int(v[h]), false);
-      const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(int(v[h]), true);
-      q[4 * h] = lo.x;
-      q[4 * h + 1] = lo.y;
-      q[4 * h + 2] = hi.x;
-      q[4 * h + 3] = hi.y;
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t p =
+          __builtin_amdgcn_perm(0u, v[i >> 1], i & 1 ? 0x030c020cu : 0x010c000cu);
+      q.h[i] = __builtin_bit_cast(f16x2, (p & 0x80008000u) | (p >> 1 & 0x3fff3fffu));
     }
+    return q;
   }
 };
 

@@ -11,8 +11,10 @@
 #include <type_traits>
 
 #include "coded.h"
+#include "coded_shapes.h"
 #include "internal.h"
 #include "shapes.h"
+#include "tiles.h"
 
 namespace cheb {
 namespace {
@@ -123,20 +125,21 @@ struct CodedResArgs {
   float *x_out;
 };
 
-// A tile is a run of 64 residual vectors of 8.  The W waves of a block share
-// it, each taking every W-th batch of U covering segments.  A segment's
-// entries are summed in fp32 (at most 8 terms), segments in fp64.
+// A tile is a run of 64 residual vectors of 8.  The W waves of a block share it,
+// each taking every W-th batch of U covering segments.  A segment's entries
+// are summed in fp32 (at most 8 terms), segments in fp64.
 template <class Fmt, int NS, int W, int U>
 __global__ __launch_bounds__(64 * W) void residual_coded_kernel(CodedResArgs<NS> a) {
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t lane = threadIdx.x & 63u;
+  const uint32_t tile = line_tile<kRuns>(blockIdx.x, gridDim.x);
   int32_t p = 0;
   for (int32_t q = 1; q < a.n_part; ++q)
-    if (blockIdx.x >= a.part[q].tile) p = q;
+    if (tile >= a.part[q].tile) p = q;
   const CodedPart part = a.part[p];
-  const uint32_t first = (blockIdx.x - part.tile) * 64u;
-  const uint32_t live = std::min(part.n_vec - first, 64u);
-  const uint32_t l = lane < live ? lane : live - 1u;  // idle lanes repeat the last
+  const uint32_t first = (tile - part.tile) * kRun;
+  const uint32_t live = std::min(part.n_vec - first, kRun);
+  const uint32_t l = std::min(lane, live - 1u);  // idle lanes repeat the last vector
   const uint64_t j0 = uint64_t(part.vec_begin) + first;
   double acc[8];
 #pragma unroll
@@ -150,17 +153,18 @@ __global__ __launch_bounds__(64 * W) void residual_coded_kernel(CodedResArgs<NS>
       const uint64_t v0 = uint64_t(a.delta[part.first + at + u]) + j0;
       const uint64_t chunk = v0 >> 12;
       uint32_t r = (uint32_t(v0) & 4095u) + l;
-      const bool next = r >= 4096u;  // 64 vectors span at most two chunks
+      const bool next = r >= 4096u;  // a run spans at most two chunks
       r &= 4095u;
       const uint32_t co = r * 8u + (next ? a.code_super : 0u);
       const uint32_t so = (r >> 9) * 128u + (r >> 2 & 15u) * 8u + (r >> 6 & 7u) +
                           (next ? a.scale_super : 0u);
 #pragma unroll
-      for (int k = 0; k < NS; ++k) {
+      for (int k = 0; k < NS; ++k)
         v[u][k] = __builtin_nontemporal_load(
             reinterpret_cast<const u32x2 *>(a.codes[k] + chunk * a.code_super + co));
+#pragma unroll
+      for (int k = 0; k < NS; ++k)
         sc[u][k] = *reinterpret_cast<const uint8_t *>(a.scales[k] + chunk * a.scale_super + so);
-      }
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -169,10 +173,9 @@ __global__ __launch_bounds__(64 * W) void residual_coded_kernel(CodedResArgs<NS>
 #pragma unroll
       for (int k = 0; k < NS; ++k) {
         const float unit = a.w[k] * __uint_as_float(sc[u][k] << 23);
-        float q[8];
-        Fmt::decode(v[u][k], q);
+        const Halves q = Fmt::decode(v[u][k]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) t[e] = k == 0 ? unit * q[e] : fmaf(unit, q[e], t[e]);
+        for (int e = 0; e < 8; ++e) t[e] = fmaf(unit, q[e], k == 0 ? 0.0f : t[e]);
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[e] += double(t[e]);
@@ -204,7 +207,7 @@ __global__ __launch_bounds__(64 * W) void residual_coded_kernel(CodedResArgs<NS>
     __syncthreads();
     for (uint32_t h = threadIdx.x; h < live * 2u; h += 64u * W) {
       const uint64_t o = j0 * 8u + 4u * h;
-      const uint32_t at = (4u * (h & 1u)) * 64u + (h >> 1);
+      const uint32_t at = 4u * (h & 1u) * 64u + (h >> 1);
       u32x4 x = {0u, 0u, 0u, 0u}, r;
       if (a.x_in) x = *reinterpret_cast<const u32x4 *>(a.x_in + o);
 #pragma unroll
@@ -229,7 +232,8 @@ struct CodedResJob {
   const float *x_in;
   float *x_out;
   const CodedPlace *place;
-  int cus;
+  int cus, lds_per_cu;
+  int waves;  // the launch shape's waves_per_cu: -1 leaves the LDS free
 };
 
 template <class Fmt, int NS>
@@ -247,20 +251,25 @@ hipError_t launch_residual_ns(const CodedResJob &j, hipStream_t s) {
   a.x_in = j.x_in;
   a.x_out = j.x_out;
   a.n_part = j.n_iv;
-  uint32_t tiles = 0;
   int ncover = 0;
+  uint32_t tiles = 0;
   for (int i = 0, first = 0; i < j.n_iv; first += j.iv[i].ncover, ++i) {
     const uint32_t n_vec = uint32_t(j.iv[i].n_vec);
     a.part[i] = CodedPart{tiles, uint32_t(j.iv[i].vec_begin), n_vec, first, j.iv[i].ncover};
-    tiles += (n_vec + 63u) / 64u;
+    tiles += run_tiles<1>(n_vec, kRunLg);
     ncover = std::max(ncover, int(j.iv[i].ncover));
   }
-  constexpr int U = NS <= 2 ? 4 : NS <= 4 ? 2 : 1;
-  if (ncover >= 8)
-    hipLaunchKernelGGL((residual_coded_kernel<Fmt, NS, 4, U>), dim3(tiles), dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL((residual_coded_kernel<Fmt, NS, 1, U>), dim3(tiles), dim3(64), 0, s, a);
-  return hipGetLastError();
+  constexpr int U = NS <= 4 ? 2 : 1;
+  const CodedResShape shape = coded_residual_shape(NS, ncover);
+  const auto launch = [&](auto kernel, int waves, size_t own) {
+    hipLaunchKernelGGL(kernel, dim3(tiles), dim3(64 * waves),
+                       residual_lds(j.lds_per_cu, shape.blocks_per_cu, own, j.waves), s, a);
+    return hipGetLastError();
+  };
+  // -- shape
+  if (shape.waves == 1) return launch(residual_coded_kernel<Fmt, NS, 1, U>, 1, 0);
+  if (shape.waves == 2) return launch(residual_coded_kernel<Fmt, NS, 2, U>, 2, 2 * 4096);
+  return launch(residual_coded_kernel<Fmt, NS, 4, U>, 4, 4 * 4096);
 }
 
 template <class Fmt>
@@ -311,9 +320,9 @@ int launch_residual_coded(int quant, int n, const CodedEntry *src, const double 
                           const int64_t *delta, int n_delta, const ResidualInterval *iv, int n_iv,
                           const float *x_in, float *x_out, const CodedPlace &place,
                           hipStream_t stream) {
-  CodedResJob j{src, w, delta, n_delta, iv, n_iv, x_in, x_out, &place, 0};
-  int lds = 0;
-  int rc = device_info(&j.cus, &lds);
+  CodedResJob j{src, w, delta, n_delta, iv, n_iv, x_in, x_out, &place, 0, 0,
+                launch_shape().waves_per_cu};
+  int rc = device_info(&j.cus, &j.lds_per_cu);
   if (rc != CHEB_OK) return rc;
   const hipError_t e = quant == CHEB_QUANT_MXINT8 ? launch_residual_fmt<Int8Fmt>(n, j, stream)
                                                   : launch_residual_fmt<E4m3Fmt>(n, j, stream);

@@ -1,0 +1,59 @@
+// How launches over 8-bit entries are laid out, by their sizes.  Host
+// arithmetic.
+#pragma once
+
+#include <stdint.h>
+
+#include <algorithm>
+
+namespace cheb {
+
+// A prediction's tiles: runs of 512 elements each, and whether the tiles that
+// share a line of scales go to one XCD.  Measured on MI355X, bf16, entries of
+// 264 M and 807 M elements in either layout, 1 to 8 entries and 1 to 4 outputs,
+// tiles of 1, 2 and 4 runs:
+//  - two runs; one where stores prevail, three outputs or more of three entries
+//    or more (6 entries, 3 outputs of 528 M: 969 us, 988 with two runs; 4
+//    entries, 4 outputs: 492, 505);
+//  - every XCD reading its own copy of a line of scales costs 9% more reads, and
+//    keeping the line's tiles together takes the stores out of their order: that
+//    pays for one output of five entries or more (6 entries of 807 M: 980 us,
+//    1009 without; 3 entries, 1 output: 201, 198 without; 6 entries, 3 outputs:
+//    1007, 969).
+struct CodedShape {
+  int runs;
+  bool lines;
+};
+constexpr CodedShape coded_shape(int ns, int no) {
+  return {no >= 3 && ns >= 3 ? 1 : 2, no == 1 && ns >= 5};
+}
+
+// One-wave blocks that share a compute unit (0: no limit).  About 76 KiB of loads
+// and stores in flight, between 8 and 20 blocks (one entry, 1 output: 120 us with 20,
+// 122 without a limit; 6 entries: 980 with 10, 1003 with 12, 1016 without); a call of
+// under 1 MiB a compute unit is over before the queues fill (3 entries of 33 M: 27.4
+// us, 28.7 with 12).
+inline int coded_blocks(int ns, int no, int out_bytes, int64_t numel, int cus) {
+  const int kib = ns + no * out_bytes;  // of 1024 elements
+  if (numel / 1024 * kib < int64_t(1024) * cus) return 0;
+  const int blocks = std::min(std::max((76 + kib / 2) / kib, 8), 20);
+  return coded_shape(ns, no).runs == 1 ? 2 * blocks : blocks;
+}
+
+// The waves that share a residual tile, and segments that one loads ahead of
+// its sums.  One segment is one wave's; a second wave pays from two on, four
+// where there is much to read (8 segments of one entry, 36.9K tiles: 50.9 us with
+// 2, 57 with 4 waves; of 4 entries 139.7, 140; 56 segments of 6 entries, FLUX-1024:
+// 784 with 4).  Five entries or more fill the queues by themselves: four blocks
+// a compute unit (FLUX-1024: 784, 797 without a limit).
+struct CodedResShape {
+  int waves;
+  int blocks_per_cu;  // 0: no limit
+};
+inline CodedResShape coded_residual_shape(int ns, int ncover) {
+  if (ncover <= 1) return {1, 0};
+  if (ncover <= 4 || (ns == 1 && ncover <= 28)) return {2, 0};
+  return {4, ns >= 5 ? 4 : 0};
+}
+
+}  // namespace cheb

@@ -202,8 +202,7 @@ struct CodedSrc {
     return h;
   }
   __device__ __forceinline__ static Four values(const Held &h) {
-    float c[8];
-    Fmt::decode(u32x2{h.codes, 0u}, c);
+    const Halves c = Fmt::decode(u32x2{h.codes, 0u});
     Four x;
 #pragma unroll
     for (int q = 0; q < 4; ++q)

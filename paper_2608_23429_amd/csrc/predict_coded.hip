@@ -6,8 +6,10 @@
 #include <string.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "coded.h"
+#include "coded_shapes.h"
 #include "internal.h"
 #include "shapes.h"
 
@@ -25,9 +27,12 @@ struct CodedHist {
 __device__ __forceinline__ float mad(float a, float b, float c) { return fmaf(a, b, c); }
 __device__ __forceinline__ double mad(double a, double b, double c) { return fma(a, b, c); }
 
+// Outputs: kLane elements of a lane, so that a store instruction of a wave
+// covers 1 KiB without gaps (fp32 outputs in stores of 32 bytes a lane with gaps
+// between them: 84 us for three entries of 66 M elements, 72 so).
 struct Bf16Out {
   using W = float;
-  static constexpr int kBytes = 2;
+  static constexpr int kLane = 8, kBytes = 2;
   __device__ __forceinline__ static void store(void *out, uint64_t e, const W (&a)[8]) {
     u32x4 r;
 #pragma unroll
@@ -41,7 +46,7 @@ struct Bf16Out {
 
 struct F16Out {
   using W = float;
-  static constexpr int kBytes = 2;
+  static constexpr int kLane = 8, kBytes = 2;
   __device__ __forceinline__ static void store(void *out, uint64_t e, const W (&a)[8]) {
     u32x4 r;
 #pragma unroll
@@ -55,67 +60,83 @@ struct F16Out {
 
 struct F32Out {
   using W = double;
-  static constexpr int kBytes = 4;
-  __device__ __forceinline__ static void store(void *out, uint64_t e, const W (&a)[8]) {
-    u32x4 *o = reinterpret_cast<u32x4 *>(static_cast<float *>(out) + e);
+  static constexpr int kLane = 4, kBytes = 4;
+  __device__ __forceinline__ static void store(void *out, uint64_t e, const W (&a)[4]) {
+    u32x4 r;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      u32x4 r;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) r[q] = __float_as_uint(float(a[4 * h + q]));
-      __builtin_nontemporal_store(r, o + h);
-    }
+    for (int q = 0; q < 4; ++q) r[q] = __float_as_uint(float(a[q]));
+    __builtin_nontemporal_store(r, reinterpret_cast<u32x4 *>(static_cast<float *>(out) + e));
   }
 };
 
-// One-wave blocks, each a tile of two runs of 64 lanes x 8 elements.
-template <class Fmt, class Out, int NS, int NO>
+template <int R>
+struct ScalesOf;
+template <>
+struct ScalesOf<1> {
+  using Type = uint8_t;
+};
+template <>
+struct ScalesOf<2> {
+  using Type = uint16_t;
+};
+
+__device__ __forceinline__ u32x2 load_codes(const u32x2 *p) {
+  return __builtin_nontemporal_load(p);
+}
+__device__ __forceinline__ u32x2 load_codes(const uint32_t *p) {
+  return u32x2{__builtin_nontemporal_load(p), 0u};
+}
+
+// One-wave blocks, each a tile of R runs of 512 elements, kLane of them to a
+// lane at a time.  kLines: the tiles that share a line of scales on one XCD.
+template <class Fmt, class Out, int NS, int NO, int R, bool kLines>
 __global__ __launch_bounds__(64) void predict_coded_kernel(
-    CodedHist<NS, NO, typename Out::W> h, uint32_t n_tiles) {
-  constexpr int R = 2;
+    CodedHist<NS, NO, typename Out::W> h) {
   using W = typename Out::W;
+  using Codes = std::conditional_t<Out::kLane == 8, u32x2, uint32_t>;
+  constexpr uint32_t V = Out::kLane, kTile = 512u * R;
+  constexpr int P = 8 / int(V);  // parts of a run, with groups of their own
+  constexpr uint32_t kChunkTiles = uint32_t(kCodedChunk) / kTile;
   const uint32_t lane = threadIdx.x;
-  // The four tiles that share a line of scales go to one XCD (blocks are
-  // dealt to the eight in turn).
-  uint32_t tile = blockIdx.x;
-  if (tile < (n_tiles & ~31u)) {
-    const uint32_t q = tile >> 3;
-    tile = ((q & ~3u) << 3) + ((tile & 7u) << 2) + (q & 3u);
-  }
-  const uint64_t chunk = tile >> 5;         // 32 tiles of 1024 elements
-  const uint32_t in = (tile & 31u) * 1024u;
-  const uint32_t co = in + lane * 8u;
-  const uint32_t so = (in >> 12) * 128u + (lane >> 2) * 8u + (in >> 9 & 7u);
-  u32x2 v[R][NS];
-  uint32_t sc[NS];
+  const uint32_t tile = kLines ? line_tile<8u / R>(blockIdx.x, gridDim.x) : blockIdx.x;
+  const uint64_t chunk = tile / kChunkTiles;
+  const uint32_t in = tile % kChunkTiles * kTile;
+  const uint64_t cb = chunk * h.code_super + in;
+  const uint64_t sb = chunk * h.scale_super + (in >> 12) * 128u + (in >> 9 & 7u);
+  u32x2 v[R * P][NS];
+  uint32_t sc[P][NS];
 #pragma unroll
-  for (int k = 0; k < NS; ++k) {
-    sc[k] = *reinterpret_cast<const uint16_t *>(h.scales[k] + chunk * h.scale_super + so);
+  for (int k = 0; k < NS; ++k)
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-      v[r][k] = __builtin_nontemporal_load(
-          reinterpret_cast<const u32x2 *>(h.codes[k] + chunk * h.code_super + co + r * 512));
-  }
+    for (int r = 0; r < R * P; ++r)
+      v[r][k] = load_codes(
+          reinterpret_cast<const Codes *>(h.codes[k] + cb + (lane * V + uint32_t(r) * 64u * V)));
+#pragma unroll
+  for (int k = 0; k < NS; ++k)
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      sc[p][k] = *reinterpret_cast<const typename ScalesOf<R>::Type *>(
+          h.scales[k] + sb + (lane * V / 32u + uint32_t(p) * (16u / P)) * 8u);
   __builtin_amdgcn_sched_barrier(0);
-  const uint64_t e0 = uint64_t(tile) * 1024u + lane * 8u;
+  const uint64_t e0 = uint64_t(tile) * kTile + lane * V;
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    W acc[NO][8];
+  for (int r = 0; r < R * P; ++r) {
+    W acc[NO][V];
 #pragma unroll
     for (int k = 0; k < NS; ++k) {
-      const W scale = W(__uint_as_float((sc[k] >> (8 * r) & 255u) << 23));
-      float q[8];
-      Fmt::decode(v[r][k], q);
+      const W scale = W(__uint_as_float((sc[r % P][k] >> (8 * (r / P)) & 255u) << 23));
+      const Halves q = Fmt::decode(v[r][k]);
 #pragma unroll
       for (int m = 0; m < NO; ++m) {
         const W unit = h.w[m][k] * scale;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          acc[m][e] = k == 0 ? unit * W(q[e]) : mad(unit, W(q[e]), acc[m][e]);
+        for (int e = 0; e < int(V); ++e)
+          acc[m][e] = mad(unit, W(q[e]), k == 0 ? W(0) : acc[m][e]);
       }
     }
 #pragma unroll
-    for (int m = 0; m < NO; ++m) Out::store(h.o[m], e0 + uint64_t(r) * 512u, acc[m]);
+    for (int m = 0; m < NO; ++m)
+      Out::store(h.o[m], e0 + uint64_t(r) * (64u * V), acc[m]);
   }
 }
 
@@ -126,6 +147,7 @@ struct Job {
   int64_t numel;
   const CodedPlace *place;
   int cus, lds_per_cu;
+  int waves;  // as configured: 0 chosen here, -1 no limit
 };
 
 template <class Fmt, class Out, int NS, int NO>
@@ -142,9 +164,14 @@ hipError_t launch_ns_no(const Job &j, hipStream_t s) {
   }
   h.code_super = j.place->code_super;
   h.scale_super = j.place->scale_super;
-  const uint32_t tiles = uint32_t(j.numel / 1024);
-  hipLaunchKernelGGL((predict_coded_kernel<Fmt, Out, NS, NO>), dim3(tiles), dim3(64), 0, s, h,
-                     tiles);
+  constexpr CodedShape kShape = coded_shape(NS, NO);
+  constexpr int R = kShape.runs;
+  // -- shape
+  const uint32_t tiles = uint32_t(j.numel / (512 * R));
+  const int blocks = j.waves != 0 ? j.waves : coded_blocks(NS, NO, Out::kBytes, j.numel, j.cus);
+  hipLaunchKernelGGL((predict_coded_kernel<Fmt, Out, NS, NO, R, kShape.lines>), dim3(tiles),
+                     dim3(64), blocks > 2 && blocks < 32 ? lds_share(j.lds_per_cu, blocks) : 0, s,
+                     h);
   return hipGetLastError();
 }
 
@@ -190,7 +217,7 @@ hipError_t launch_fmt(int dtype, int n, int n_out, const Job &j, hipStream_t s) 
 int launch_predict_coded(int quant, int dtype, const CodedEntry *src, int n, const double *w,
                          int n_out, void *const *out, int64_t numel, const CodedPlace &place,
                          hipStream_t stream) {
-  Job j{src, w, out, numel, &place, 0, 0};
+  Job j{src, w, out, numel, &place, 0, 0, launch_shape().waves_per_cu};
   int rc = device_info(&j.cus, &j.lds_per_cu);
   if (rc != CHEB_OK) return rc;
   const hipError_t e = quant == CHEB_QUANT_MXINT8 ? launch_fmt<Int8Fmt>(dtype, n, n_out, j, stream)
