@@ -136,12 +136,20 @@ struct CodedResArgs {
 
 // A tile is a run of 64 residual vectors of 8.  The W waves of a block share it,
 // each taking every W-th batch of U covering segments.  A segment's entries
-// are summed in fp32 (at most 8 terms), segments in fp64.
+// are summed in fp32 (at most 8 terms), segments in fp64, the waves' sums
+// through LDS.  Bound by HBM reads: 33 bytes for 32 elements of each entry and
+// segment.  FLUX-1024, 6 interleaved entries: 785 us, 6.5 TB/s; without its
+// scales it takes 733, so the lines of scales, 1 in 33, cost 7%: each is read by
+// 8 tiles, which are kept on one XCD for that, with those of the next line (797
+// where every XCD reads its own).  Tried and left: 16 elements to a lane, which
+// halves the load instructions (785; DiT 256 19.1 -> 21.3), entries' lines
+// of a block side by side (788, three-target predictions 3% slower), lines next
+// to their codes (858).
 template <class Fmt, int NS, int W, int U>
 __global__ __launch_bounds__(64 * W) void residual_coded_kernel(CodedResArgs<NS> a) {
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t lane = threadIdx.x & 63u;
-  const uint32_t tile = line_tile<kRuns>(blockIdx.x, gridDim.x);
+  const uint32_t tile = line_tile<2 * kRuns>(blockIdx.x, gridDim.x);
   int32_t p = 0;
   for (int32_t q = 1; q < a.n_part; ++q)
     if (tile >= a.part[q].tile) p = q;
@@ -268,7 +276,7 @@ hipError_t launch_residual_ns(const CodedResJob &j, hipStream_t s) {
     tiles += run_tiles<1>(n_vec, kRunLg);
     ncover = std::max(ncover, int(j.iv[i].ncover));
   }
-  constexpr int U = NS <= 4 ? 2 : 1;
+  constexpr int U = 2;  // segments ahead of their sums
   const CodedResShape shape = coded_residual_shape(NS, ncover);
   const auto launch = [&](auto kernel, int waves, size_t own) {
     hipLaunchKernelGGL(kernel, dim3(tiles), dim3(64 * waves),
@@ -278,7 +286,8 @@ hipError_t launch_residual_ns(const CodedResJob &j, hipStream_t s) {
   // -- shape
   if (shape.waves == 1) return launch(residual_coded_kernel<Fmt, NS, 1, U>, 1, 0);
   if (shape.waves == 2) return launch(residual_coded_kernel<Fmt, NS, 2, U>, 2, 2 * 4096);
-  return launch(residual_coded_kernel<Fmt, NS, 4, U>, 4, 4 * 4096);
+  if (shape.waves == 4) return launch(residual_coded_kernel<Fmt, NS, 4, U>, 4, 4 * 4096);
+  return launch(residual_coded_kernel<Fmt, NS, 8, U>, 8, 8 * 4096);
 }
 
 template <class Fmt>

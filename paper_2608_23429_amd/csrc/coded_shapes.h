@@ -40,12 +40,14 @@ inline int coded_blocks(int ns, int no, int out_bytes, int64_t numel, int cus) {
   return coded_shape(ns, no).runs == 1 ? 2 * blocks : blocks;
 }
 
-// The waves that share a residual tile, and segments that one loads ahead of
-// its sums.  One segment is one wave's; a second wave pays from two on, four
-// where there is much to read (8 segments of one entry, 36.9K tiles: 50.9 us with
-// 2, 57 with 4 waves; of 4 entries 139.7, 140; 56 segments of 6 entries, FLUX-1024:
-// 784 with 4).  Five entries or more fill the queues by themselves: four blocks
-// a compute unit (FLUX-1024: 784, 797 without a limit).
+// The waves that share a residual tile; each loads two segments ahead of its
+// sums.  One segment is one wave's; a second wave pays from two on (2 segments
+// of one entry, 36.9K tiles: 33.3 us, 37.0 with one), four where there is much to
+// read (24 segments of 2 entries, 1152 tiles: 7.9 us, 8.5 with two; 8 segments of
+// one entry: 50.9 with two, 57 with four), and eight for many segments of three
+// entries or more (DiT-XL/2 256, 56 segments of 3 entries: 19.1, 20.3 with four).
+// Five entries or more fill the queues by themselves: 16 waves a compute unit
+// (FLUX-1024: 785, 797 without a limit).
 struct CodedResShape {
   int waves;
   int blocks_per_cu;  // 0: no limit
@@ -53,6 +55,7 @@ struct CodedResShape {
 inline CodedResShape coded_residual_shape(int ns, int ncover) {
   if (ncover <= 1) return {1, 0};
   if (ncover <= 4 || (ns == 1 && ncover <= 28)) return {2, 0};
+  if (ns >= 3 && ncover >= 24) return {8, ns >= 5 ? 2 : 0};
   return {4, ns >= 5 ? 4 : 0};
 }
 
