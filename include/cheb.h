@@ -620,7 +620,7 @@ enum { CHEB_OUT_MXFP8 = 16, CHEB_OUT_FP8_ROW = 17 };
  *                    2^34, rows below 2^26.
  *   kind             CHEB_NORM_RMS or CHEB_NORM_LAYER.
  *   x_dtype          cheb_dtype of x_in and x_out.
- *   eps              finite, >= 0.
+ *   eps              finite, >= 0; with 0 a row of zeros is NaN.
  *   x_in             [rows][dim], or NULL (zero).
  *   x_out            [rows][dim], or NULL (x is not kept).  It may be x_in.
  *   gain, shift      fp32 [groups][dim], each may be NULL (one, zero); row r
@@ -698,7 +698,8 @@ CHEB_API int cheb_residual_norm(cheb_cache *c, const double *w, int32_t seg, int
  *                taken; -1 leaves it free.  The residual calls reserve LDS in
  *                the same way, up to all of it, under limits of their own;
  *                -1 leaves them only what their sums take (at most 64 KiB a
- *                block), other values do not reach them.
+ *                block), other values do not reach them.  Predictions from
+ *                8-bit entries take the cap (or -1) and choose the rest.
  * Default {64, 1, 1, 0, 0}.  On MI355X a bf16 history of 5-6 entries
  * streams at 0.83 (contiguous) to 0.87 (interleaved) of the HBM peak under
  * the chosen cap, against 0.75 with 1024-thread blocks at full occupancy:

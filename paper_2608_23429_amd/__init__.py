@@ -225,6 +225,14 @@ def _here(t, what: str, current: int):
                     f"{what} is on {t.device}, the current device is {current}")
 
 
+def _stream_here(stream: Optional[torch.cuda.Stream], current: int) -> int:
+    """A stream of the current device."""
+    if stream is not None and stream.device.index != current:
+        raise ChebError(_binding.CHEB_E_INVAL,
+                        f"the stream is on {stream.device}, the current device is {current}")
+    return _stream_handle(stream, current)
+
+
 def _norm_rows(t, what: str, dim: int, rows: int) -> int:
     """Groups of a gain or shift."""
     n = t.numel()
@@ -316,7 +324,7 @@ def add_norm(srcs: Sequence[torch.Tensor], w, x_out: Optional[torch.Tensor] = No
         dim = like.shape[-1] if like.dim() else 1
     norm, out = _norm_call(current, like.device, x_out, x_in, numel, dim, kind, eps, gain, shift,
                            out)
-    cheb_add_norm(ptrs, w, cheb_dtype(dtype), norm, _stream_handle(stream, current))
+    cheb_add_norm(ptrs, w, cheb_dtype(dtype), norm, _stream_here(stream, current))
     return x_out, out
 
 
@@ -467,6 +475,19 @@ class ChebCache:
     def handle(self):
         return self._h
 
+    def _check_here(self, stream: Optional[torch.cuda.Stream], *tensors: torch.Tensor):
+        """Work on 8-bit entries goes to the current device: the cache, the
+        stream and the tensors are all on it."""
+        current = torch.cuda.current_device()
+        if self.device.index != current or (stream is not None
+                                            and stream.device.index != current):
+            raise ChebError(_binding.CHEB_E_INVAL, f"the cache ({self.device}) or the stream is "
+                            f"not on the current device, {current}")
+        for t in tensors:
+            if t.get_device() != current:
+                raise ChebError(_binding.CHEB_E_INVAL, f"a tensor is on {t.device}, the cache "
+                                f"on {self.device}")
+
     # -- buffers -------------------------------------------------------------
     def new_output(self) -> torch.Tensor:
         return torch.empty(self.slot_numel, dtype=self.dtype, device=self.device)
@@ -510,6 +531,8 @@ class ChebCache:
         own, whatever the layout; of 8-bit entries the values of the codes."""
         out = self.new_output() if out is None else out
         self._check_out(out)
+        if self.quant is not None:
+            self._check_here(stream, out)
         cheb_cache_read(self._h, idx, out.data_ptr(), _stream_handle(stream))
         return out
 
@@ -526,6 +549,8 @@ class ChebCache:
                 raise ChebError(_binding.CHEB_E_MISMATCH,
                                 f"segments[{len(ptrs)}] differs from the layout")
             ptrs.append(s.data_ptr())
+        if self.quant is not None:
+            self._check_here(stream, *segments)
         cheb_cache_push(self._h, t, ptrs, _stream_handle(stream))
 
     def begin_push(self) -> torch.Tensor:
@@ -555,6 +580,8 @@ class ChebCache:
                     stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         out = self.new_output() if out is None else out
         self._check_out(out)
+        if self.quant is not None:
+            self._check_here(stream, out)
         cheb_extrapolate(self._h, w, out.data_ptr(), _stream_handle(stream))
         return out
 
@@ -564,7 +591,10 @@ class ChebCache:
         outs = [self.new_output() for _ in range(w.shape[0])] if outs is None else list(outs)
         for o in outs:
             self._check_out(o)
-        cheb_extrapolate_multi(self._h, w, [o.data_ptr() for o in outs], _stream_handle(stream))
+        if self.quant is not None:
+            self._check_here(stream, *outs)
+        cheb_extrapolate_multi(self._h, w, [o.data_ptr() for o in outs],
+                               _stream_handle(stream))
         return outs
 
     def extrapolate_at_multi(self, targets, outs: Optional[Sequence[torch.Tensor]] = None,
@@ -573,6 +603,8 @@ class ChebCache:
         outs = [self.new_output() for _ in targets] if outs is None else list(outs)
         for o in outs:
             self._check_out(o)
+        if self.quant is not None:
+            self._check_here(stream, *outs)
         w = cheb_extrapolate_at_multi(self._h, targets, [o.data_ptr() for o in outs],
                                       _stream_handle(stream), n_slots=self.n_slots)
         return outs, w
@@ -583,6 +615,8 @@ class ChebCache:
         outs = [self.new_output() for _ in range(n_steps)] if outs is None else list(outs)
         for o in outs:
             self._check_out(o)
+        if self.quant is not None:
+            self._check_here(stream, *outs)
         cheb_extrapolate_steps(self._h, table.handle, first_step, [o.data_ptr() for o in outs],
                                _stream_handle(stream))
         return outs
@@ -598,6 +632,8 @@ class ChebCache:
             _check_device_tensor(x_in, "x_in")
             if x_in.dtype != torch.float32 or x_in.numel() != x_out.numel():
                 raise ChebError(_binding.CHEB_E_MISMATCH, "x_in differs from x_out")
+        if self.quant is not None:
+            self._check_here(stream, x_out, x_out if x_in is None else x_in)
         cheb_residual_apply(self._h, w, res_offset, x_out.numel(),
                             None if x_in is None else x_in.data_ptr(), x_out.data_ptr(),
                             _stream_handle(stream))
@@ -624,13 +660,15 @@ class ChebCache:
         _here(self.arena, "the cache", current)
         norm, out = _norm_call(current, self.device, x_out, x_in, rows * dim, dim, kind, eps, gain,
                                shift, out)
-        cheb_residual_norm(self._h, w, seg, first, norm, _stream_handle(stream, current))
+        cheb_residual_norm(self._h, w, seg, first, norm, _stream_here(stream, current))
         return x_out, out
 
     def extrapolate_at(self, target_t: float, out: Optional[torch.Tensor] = None,
                        stream: Optional[torch.cuda.Stream] = None):
         out = self.new_output() if out is None else out
         self._check_out(out)
+        if self.quant is not None:
+            self._check_here(stream, out)
         w = cheb_extrapolate_at(self._h, target_t, out.data_ptr(), _stream_handle(stream),
                                 n_slots=self.n_slots)
         return out, w

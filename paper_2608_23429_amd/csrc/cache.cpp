@@ -339,7 +339,7 @@ int cheb_cache_push(cheb_cache *c, double t, const void *const *seg_src, void *s
   // part of the slot cannot leave a half-overwritten entry in the history.
   const int32_t slot = claim_slot(c);
   if (c->coded)
-    rc = c->coded->push(c, slot, seg_src, static_cast<hipStream_t>(stream));
+    rc = c->coded->push(c, slot, segs.data(), int(n_segs), static_cast<hipStream_t>(stream));
   else
     rc = launch_gather(c->dtype, c->slot_ptr(slot), segs.data(), int(n_segs), c->super_vecs,
                        static_cast<hipStream_t>(stream));

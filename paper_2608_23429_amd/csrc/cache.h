@@ -10,7 +10,7 @@ namespace cheb {
 // What a ring of 8-bit entries (coded.cpp) does in place of a plain one.
 // Arguments are validated by the calls that reach these.
 struct CodedOps {
-  int (*push)(const cheb_cache *c, int32_t slot, const void *const *seg_src, hipStream_t stream);
+  int (*push)(const cheb_cache *c, int32_t slot, GatherSeg *segs, int n_segs, hipStream_t stream);
   // From the `used` newest entries but for `skip` of them, oldest first.
   int (*predict)(const cheb_cache *c, int32_t skip, int32_t used, const double *w, int32_t n_out,
                  void *const *out, hipStream_t stream);

@@ -5,6 +5,7 @@
 #include <math.h>
 #include <string.h>
 
+#include <memory>
 #include <new>
 #include <vector>
 
@@ -78,13 +79,8 @@ CodedEntry entry_of(const cheb_cache *c, int32_t slot) {
           c->place.scales + size_t(slot) * c->place.scale_lane};
 }
 
-int push(const cheb_cache *c, int32_t slot, const void *const *seg_src, hipStream_t stream) {
-  const size_t n = c->seg_numel.size();
-  std::vector<GatherSeg> segs(n);
-  for (size_t s = 0; s < n; ++s)
-    segs[s] = GatherSeg{seg_src[s], c->seg_offset[s], c->seg_numel[s]};
-  return launch_store(c->quant, c->dtype, entry_of(c, slot), c->place, segs.data(), int(n),
-                      stream);
+int push(const cheb_cache *c, int32_t slot, GatherSeg *segs, int n_segs, hipStream_t stream) {
+  return launch_store(c->quant, c->dtype, entry_of(c, slot), c->place, segs, n_segs, stream);
 }
 
 int predict(const cheb_cache *c, int32_t skip, int32_t used, const double *w, int32_t n_out,
@@ -117,7 +113,8 @@ extern "C" {
 
 int cheb_cache_layout_quant(int32_t n_slots, int32_t dtype, int32_t quant,
                             const int64_t *seg_numel, int32_t n_segs, int32_t layout,
-                            int64_t *seg_offset, int64_t *slot_numel, size_t *arena_bytes) {
+                            int64_t *seg_offset, int64_t *slot_numel,
+                            size_t *arena_bytes) try {
   Layout l;
   int rc = lay_out(n_slots, dtype, quant, seg_numel, n_segs, layout, &l);
   if (rc != CHEB_OK) return rc;
@@ -125,11 +122,13 @@ int cheb_cache_layout_quant(int32_t n_slots, int32_t dtype, int32_t quant,
   if (slot_numel) *slot_numel = l.slot_numel;
   if (arena_bytes) *arena_bytes = l.bytes;
   return ok();
+} catch (const std::bad_alloc &) {
+  return fail(CHEB_E_INVAL, "out of host memory");
 }
 
 int cheb_cache_create_quant(cheb_cache **out, int32_t n_slots, int32_t dtype, int32_t quant,
                             const int64_t *seg_numel, int32_t n_segs, int32_t layout, void *arena,
-                            size_t arena_bytes) {
+                            size_t arena_bytes) try {
   if (!out) return fail(CHEB_E_INVAL, "out is NULL");
   *out = nullptr;
   Layout l;
@@ -141,8 +140,7 @@ int cheb_cache_create_quant(cheb_cache **out, int32_t n_slots, int32_t dtype, in
   if (arena_bytes < l.bytes)
     return fail(CHEB_E_MISMATCH, "arena holds %zu bytes, the layout needs %zu", arena_bytes,
                 l.bytes);
-  cheb_cache *c = new (std::nothrow) cheb_cache();
-  if (!c) return fail(CHEB_E_INVAL, "out of host memory");
+  std::unique_ptr<cheb_cache> c(new cheb_cache());
   c->n_slots = n_slots;
   c->dtype = dtype;
   c->seg_numel.assign(seg_numel, seg_numel + n_segs);
@@ -160,8 +158,10 @@ int cheb_cache_create_quant(cheb_cache **out, int32_t n_slots, int32_t dtype, in
                      : c->arena;
   c->place.codes = region + l.codes;
   c->place.scales = region + l.scales;
-  *out = c;
+  *out = c.release();
   return ok();
+} catch (const std::bad_alloc &) {
+  return fail(CHEB_E_INVAL, "out of host memory");
 }
 
 int cheb_cache_quant(const cheb_cache *c, int32_t *quant) {

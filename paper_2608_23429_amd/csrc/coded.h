@@ -119,7 +119,7 @@ struct E4m3Fmt {
   static constexpr uint32_t kLimitFraction = 0x600000u;  // 448 = 1.75 2^8
   static constexpr int kLimitExponent = 8;
   static constexpr int kShift = 0;
-  static constexpr double kUnit = 0x1p8;
+  static constexpr double kUnit = 1.0;
 
   __device__ __forceinline__ static u32x2 encode(const float (&x)[8], const Group &g) {
     float v[8];
@@ -142,14 +142,16 @@ struct E4m3Fmt {
 
   // The code's exponent and fraction one place below a half's sign are the
   // fp16 number of 2^-8 its value (exponents are biased by 7 and 15), fp16's
-  // small numbers being e4m3's.  Codes are never NaN.
+  // small numbers being e4m3's.  Codes are never NaN.  The 2^8 is not left to
+  // the weights: with a scale of 2^120 they would overflow.
   __device__ __forceinline__ static Halves decode(u32x2 v) {
+    const f16x2 up = {_Float16(256.0f), _Float16(256.0f)};
     Halves q;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t p =
           __builtin_amdgcn_perm(0u, v[i >> 1], i & 1 ? 0x030c020cu : 0x010c000cu);
-      q.h[i] = __builtin_bit_cast(f16x2, (p & 0x80008000u) | (p >> 1 & 0x3fff3fffu));
+      q.h[i] = __builtin_bit_cast(f16x2, (p & 0x80008000u) | (p >> 1 & 0x3fff3fffu)) * up;
     }
     return q;
   }

@@ -277,7 +277,7 @@ hipError_t launch_residual_ns(const CodedResJob &j, hipStream_t s) {
     ncover = std::max(ncover, int(j.iv[i].ncover));
   }
   constexpr int U = 2;  // segments ahead of their sums
-  const CodedResShape shape = coded_residual_shape(NS, ncover);
+  const CodedResShape shape = coded_residual_shape(NS, ncover, tiles);
   const auto launch = [&](auto kernel, int waves, size_t own) {
     hipLaunchKernelGGL(kernel, dim3(tiles), dim3(64 * waves),
                        residual_lds(j.lds_per_cu, shape.blocks_per_cu, own, j.waves), s, a);

@@ -52,7 +52,9 @@ struct CodedResShape {
   int waves;
   int blocks_per_cu;  // 0: no limit
 };
-inline CodedResShape coded_residual_shape(int ns, int ncover) {
+inline CodedResShape coded_residual_shape(int ns, int ncover, uint32_t tiles) {
+  // HIP refuses a grid of 2^32 threads, which 8 waves a tile reach at 2^23.
+  if (tiles >= uint32_t(1) << 23) return {1, 0};
   if (ncover <= 1) return {1, 0};
   if (ncover <= 4 || (ns == 1 && ncover <= 28)) return {2, 0};
   if (ns >= 3 && ncover >= 24) return {8, ns >= 5 ? 2 : 0};

@@ -109,6 +109,74 @@ def test_store_largest():
     cache.close()
 
 
+@pytest.mark.parametrize("quant", QUANTS)
+def test_store_near_the_largest(quant):
+    """Beside fp32's largest values small ones and zeros keep their own: a scale
+    of 2^120 or more takes no other factor past the range."""
+    x = torch.zeros(96)
+    x[0], x[1], x[2] = 3.0e38, -2.9e38, 1.0
+    x[40] = 1.5e38
+    x[70] = torch.finfo(torch.float32).max
+    cache = cheb.ChebCache(1, torch.float32, [96], quant=quant)
+    cache.push(0.0, [x.cuda()])
+    with np.errstate(over="ignore"):
+        want = ref.held(f64(x), quant).astype(np.float32).astype(np.float64)
+    np.testing.assert_array_equal(f64(cache.read(0))[:96], want)
+    np.testing.assert_array_equal(f64(cache.extrapolate([1.0]))[:96], want)
+    cache.close()
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_read_plain_cache(dtype, layout):
+    """cheb_cache_read gives a plain cache's entries bit for bit."""
+    steps = [values(RAGGED, dtype, 3 + k) for k in range(3)]
+    cache = cheb.ChebCache(2, DTYPES[dtype], RAGGED, layout=layout)
+    fill(cache, steps)
+    for idx in range(2):
+        got = cache.read(idx)
+        assert torch.equal(got.view(torch.uint8), cache.entry(idx).contiguous().view(torch.uint8))
+        for v, s in zip(cache.segment_views(got), steps[1 + idx]):
+            assert torch.equal(v.cpu(), s)
+    cache.close()
+
+
+@pytest.mark.parametrize("quant", QUANTS)
+def test_one_group_not_finite(quant):
+    """A NaN stays in its group of 32 through predictions and residual updates,
+    whatever its entry's weight."""
+    steps = [values([4096], "bf16", k) for k in range(2)]
+    steps[0][0][100] = float("nan")
+    cache = cheb.ChebCache(2, torch.bfloat16, [4096], quant=quant)
+    fill(cache, steps)
+    x = torch.randn(4096, device="cuda")
+    for w in ([0.0, 1.0], [2.0, -1.0]):
+        out = f64(cache.extrapolate(w))
+        res = f64(cache.residual_apply(w, [0], torch.empty_like(x), x))
+        for v in (out, res):
+            assert np.isnan(v[96:128]).all() and np.isfinite(np.delete(v, slice(96, 128))).all()
+    cache.close()
+
+
+@pytest.mark.parametrize("waves", [-1, 3, 9])
+def test_launch_config_reaches_coded(waves):
+    """The tuning interface's cap changes no result."""
+    steps = [values([300000], "bf16", k) for k in range(3)]
+    cache = cheb.ChebCache(3, torch.bfloat16, [300000], quant="mxint8", layout="interleaved")
+    fill(cache, steps)
+    x = torch.randn(300000, device="cuda")
+    want = [cache.extrapolate([1.0, -2.0, 3.0]),
+            cache.residual_apply([1.0, -2.0, 3.0], [0], torch.empty_like(x), x)]
+    try:
+        cheb.cheb_set_launch_config(**dict(cheb.DEFAULT_LAUNCH_CONFIG, waves_per_cu=waves))
+        assert torch.equal(cache.extrapolate([1.0, -2.0, 3.0]), want[0])
+        assert torch.equal(cache.residual_apply([1.0, -2.0, 3.0], [0], torch.empty_like(x), x),
+                           want[1])
+    finally:
+        cheb.cheb_set_launch_config(**cheb.DEFAULT_LAUNCH_CONFIG)
+    cache.close()
+
+
 def rows(n, m, seed):
     return np.random.default_rng(seed).normal(size=(m, n)) * 3
 

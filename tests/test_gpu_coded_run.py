@@ -190,6 +190,15 @@ def test_other_device_refused(monkeypatch):
     with pytest.raises(cheb.ChebError) as e:
         cheb.add_norm([], [], x, x, out=torch.empty_like(x))
     assert e.value.name == "CHEB_E_INVAL"
+    cache = cheb.ChebCache(1, torch.float32, [256], device=x.device, quant="mxint8")
+    for call in (lambda: cache.push(0.0, [x]), lambda: cache.read(0),
+                 lambda: cache.extrapolate([1.0]), lambda: cache.extrapolate_multi([[1.0]]),
+                 lambda: cache.extrapolate_at(0.5), lambda: cache.extrapolate_at_multi([0.5]),
+                 lambda: cache.residual_apply([1.0], [0], x),
+                 lambda: cache.residual_norm([1.0], 0, dim=64)):
+        with pytest.raises(cheb.ChebError) as e:
+            call()
+        assert e.value.name == "CHEB_E_INVAL" and "current device" in str(e.value)
 
 
 def test_python_refuses():
