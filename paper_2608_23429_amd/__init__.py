@@ -250,15 +250,17 @@ def _norm_call(current, device, x_out, x_in, numel, dim, kind, eps, gain, shift,
     in_ptr = out_ptr = gain_ptr = shift_ptr = scale_ptr = None
     if x_in is not None:
         _here(x_in, "x_in", current)
-        in_ptr, x_dt = x_in.data_ptr(), cheb_dtype(x_in.dtype)
+        in_ptr, x_dt = x_in.data_ptr(), _DTYPES.get(x_in.dtype)
         if x_in.numel() != numel:
             raise ChebError(_binding.CHEB_E_MISMATCH,
                             f"x_in holds {x_in.numel()} elements, the sources {numel}")
     if x_out is not None:
         _here(x_out, "x_out", current)
-        out_ptr, x_dt = x_out.data_ptr(), cheb_dtype(x_out.dtype)
+        out_ptr, x_dt = x_out.data_ptr(), _DTYPES.get(x_out.dtype)
         if x_out.numel() != numel or (x_in is not None and x_in.dtype is not x_out.dtype):
             raise ChebError(_binding.CHEB_E_MISMATCH, "x_out differs from x_in or the sources")
+    if x_dt is None:
+        raise ChebError(_binding.CHEB_E_DTYPE, "unsupported dtype of the residual")
     if dim < 1 or numel % dim:
         raise ChebError(_binding.CHEB_E_MISMATCH, f"{numel} elements are no rows of {dim}")
     rows, groups = numel // dim, 0
@@ -274,9 +276,9 @@ def _norm_call(current, device, x_out, x_in, numel, dim, kind, eps, gain, shift,
         if gain is not None and of_shift != groups:
             raise ChebError(_binding.CHEB_E_MISMATCH, "gain and shift differ in groups")
         groups = of_shift
-    if isinstance(out, (str, torch.dtype)):
+    if type(out) is str or type(out) is torch.dtype:
         out = norm_output(rows, dim, out, device)
-    if isinstance(out, tuple):
+    if type(out) is tuple:
         y, scale = out
         _here(scale, "out's scales", current)
         scale_ptr = scale.data_ptr()
@@ -286,8 +288,9 @@ def _norm_call(current, device, x_out, x_in, numel, dim, kind, eps, gain, shift,
                 or (fmt == CHEB_OUT_MXFP8 and scale.dtype is not torch.float8_e8m0fnu)):
             raise ChebError(_binding.CHEB_E_MISMATCH, "out differs from norm_output's")
     else:
-        y = out
-        fmt = cheb_dtype(y.dtype)
+        y, fmt = out, _DTYPES.get(out.dtype)
+        if fmt is None:
+            raise ChebError(_binding.CHEB_E_DTYPE, f"unsupported dtype {y.dtype}")
     _here(y, "out", current)
     if y.numel() != numel:
         raise ChebError(_binding.CHEB_E_MISMATCH, f"out holds {y.numel()} elements, not {numel}")
