@@ -339,8 +339,8 @@ def prepare(case, seed):
                 s["cache"] = cache
             elif c["source"] == "collapsed":
                 hist = cheb.ResidualHistory(c["n"], [0], x.numel())
-                for step, v in zip(nodes, srcs):
-                    hist.push(_x(step), [v])
+                for step, v in zip(nodes, srcs):  # entries of any size, as they are
+                    hist.cache.push(_x(step), [v])
                 s["hist"] = hist
         return s
     segs = _segments(c)
