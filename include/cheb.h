@@ -592,11 +592,12 @@ CHEB_API int cheb_residual_reduce(const void *const *seg_src, const int64_t *seg
  * block that is computed or the final layer, normalises it first.  These calls
  * form the updated residual and its norm in one pass.  For each of `rows` rows
  * of `dim` elements:
- *     x = x_in + sum_k w_k s_k   (fp64 for fp32 sources, else fp32)
+ *     x = x_in + sum_k w_k s_k
  *     h = x - mean(x)   (CHEB_NORM_LAYER), x       (CHEB_NORM_RMS)
  *     y = h / sqrt(mean(h^2) + eps) * gain + shift
- * x_out receives x rounded to x_dtype; y is formed from x before that rounding,
- * its means and h in fp64, the rest in fp32, and rounded once to out_format. */
+ * x_out receives x, formed in fp64, rounded to fp32 and to x_dtype.  y is formed
+ * from x before that: h / sqrt(..) in fp64, rounded to fp32, gain and shift in
+ * fp32, and rounded once to out_format. */
 enum { CHEB_NORM_RMS = 0, CHEB_NORM_LAYER = 1 };
 
 /* Output formats of y besides the storage types, both of e4m3 codes:
@@ -658,7 +659,7 @@ CHEB_API int cheb_add_norm(const void *const *src, int32_t n_src, const double *
  * output of that module, or with a collapsed history the block stack's whole
  * contribution).  Any cache, of either layout and of 8-bit entries too.
  *   w    [n_slots] host fp64, aligned with cheb_cache_history.
- * Requires a full history.  Over fp32 entries an fp32 x_out equals, bit for bit,
+ * Requires a full history.  Over plain entries an fp32 x_out equals, bit for bit,
  * cheb_residual_apply's with that segment alone.  Errors: CHEB_E_INVAL (also a range past the tensor),
  * CHEB_E_NOTREADY, CHEB_E_DTYPE, CHEB_E_ALIGN, CHEB_E_NONFINITE, CHEB_E_HIP. */
 CHEB_API int cheb_residual_norm(cheb_cache *c, const double *w, int32_t seg, int64_t first,

@@ -283,7 +283,6 @@ hipError_t launch_residual_ns(const CodedResJob &j, hipStream_t s) {
                        residual_lds(j.lds_per_cu, shape.blocks_per_cu, own, j.waves), s, a);
     return hipGetLastError();
   };
-  // -- shape
   if (shape.waves == 1) return launch(residual_coded_kernel<Fmt, NS, 1, U>, 1, 0);
   if (shape.waves == 2) return launch(residual_coded_kernel<Fmt, NS, 2, U>, 2, 2 * 4096);
   if (shape.waves == 4) return launch(residual_coded_kernel<Fmt, NS, 4, U>, 4, 4 * 4096);

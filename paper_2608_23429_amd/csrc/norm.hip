@@ -146,7 +146,6 @@ struct PlainSrc {
   using At = uint32_t;                                      // bytes from the row's base
   static constexpr uint32_t kLg = DT == CHEB_F32 ? 13 : 14;  // elements of a chunk
   static constexpr bool kAnyPlace = true;                    // fours may start at any element
-  using Sum = std::conditional_t<DT == CHEB_F32, double, float>;
 
   __device__ __forceinline__ static RowAt row(const NormArgs &a, uint64_t e) {
     if (!a.chunked) return {e * Type::kSize, 0u, 0u};
@@ -183,7 +182,6 @@ struct CodedSrc {
     uint32_t code, scale;
   };
   static constexpr bool kAnyPlace = false;
-  using Sum = float;
 
   __device__ __forceinline__ static RowAt row(const NormArgs &a, uint64_t e) {
     return {(e >> kCodedChunkLg) * a.super, (e >> kCodedChunkLg) * a.scale_super,
@@ -318,12 +316,9 @@ __device__ __forceinline__ void store_rows(void *to, uint64_t r0, const Four (&x
       store_four<DT, M != kEven, kStream>(p + int64_t(int32_t(el[i])) * Stored<DT>::kSize, x[i], own[i]);
 }
 
-__device__ __forceinline__ float mad(float a, float b, float c) { return fmaf(a, b, c); }
-__device__ __forceinline__ double mad(double a, double b, double c) { return fma(a, b, c); }
-
 // sum = x_in + the sources' sum, kept where that is asked for.
-template <int DT, int P, int M, class Sum>
-__device__ __forceinline__ void add_rows(Sum (&sum)[P][4], const Raw (&x0)[P], void *to,
+template <int DT, int P, int M>
+__device__ __forceinline__ void add_rows(double (&sum)[P][4], const Raw (&x0)[P], void *to,
                                          uint64_t r0, const uint32_t (&el)[P],
                                          const Own (&own)[P]) {
   Four x[P];
@@ -332,7 +327,7 @@ __device__ __forceinline__ void add_rows(Sum (&sum)[P][4], const Raw (&x0)[P], v
     x[i] = Stored<DT>::values(x0[i]);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      sum[i][q] = Sum(x[i].v[q]) + sum[i][q];
+      sum[i][q] = double(x[i].v[q]) + sum[i][q];
       x[i].v[q] = float(sum[i][q]);
     }
   }
@@ -342,15 +337,16 @@ __device__ __forceinline__ void add_rows(Sum (&sum)[P][4], const Raw (&x0)[P], v
 // One pass: L threads hold a row in registers, P times four elements each (thread
 // t's i-th four is elements (i L + t) * 4 on), so that x is formed, summed and
 // normed without being read again; B sources are loaded ahead of their sums.
-// Bound by HBM: n sources and x_in read, x_out and y written.  fp64 where it
-// matters: sums of fp32 sources, and the squares and means, whose fp32 sums
-// could overflow or cancel.  Conversions from and to fp64 run at a quarter of
-// the rate, so 16- and 8-bit sources, whose predictions are summed in fp32
-// too, keep to that.  Sources carry the non-temporal hint, and so does x_out,
-// which is read a whole block later; x_in may be in a cache still, and y is
-// read next.  Measured on MI355X:
-//   8192 x 1152, 6 bf16 entries into MXFP8: 32.4 us, 6.1 TB/s (39.6 without the
-//   hints); 16384 x 1152, layer norm of 4 fp32 entries: 74.4 us, 6.4 TB/s (88);
+// Bound by HBM: n sources and x_in read, x_out and y written.  x, its mean and
+// squares and the product with the row's factor are fp64, whose sums neither
+// overflow nor cancel, so y is rounded to fp32 once before its gain and shift:
+// an 8-bit code then flips beside a tie less often than it would by an fp32
+// chain.  (All of it in fp32 for 16- and 8-bit sources: 0 to 9% less time; 16384 x
+// 1152, one bf16 source, layer norm 27.8 us for 29.6.)  Sources carry the non-temporal hint, and so
+// does x_out, which is read a whole block later; x_in may be in a cache still,
+// and y is read next.  Measured on MI355X:
+//   8192 x 1152, 6 bf16 entries into MXFP8: 33.0 us, 6.0 TB/s (39.6 without the
+//   hints); 16384 x 1152, layer norm of 4 fp32 entries: 75.8 us, 6.2 TB/s (88);
 //   5003 x 1155 in fp16, a scale a row: 10.9 us.
 template <class Src, int L, int P, int B, int M>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a) {
@@ -388,12 +384,11 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a) {
 #pragma unroll
     for (int i = 0; i < P; ++i) at[i] = Src::at(a, from, el[i]);
   }
-  using Sum = typename Src::Sum;
-  Sum acc[P][4];
+  double acc[P][4];
 #pragma unroll
   for (int i = 0; i < P; ++i)
 #pragma unroll
-    for (int q = 0; q < 4; ++q) acc[i][q] = Sum(-0.0);  // the sum of nothing: x + -0.0 is x, -0.0 too
+    for (int q = 0; q < 4; ++q) acc[i][q] = -0.0;  // the sum of nothing: x + -0.0 is x, -0.0 too
   Raw x0[P];
 #pragma unroll
   for (int i = 0; i < P; ++i) x0[i] = Raw{{0u, 0u, 0u, 0u}};
@@ -426,12 +421,12 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a) {
 #pragma unroll
     for (int j = 0; j < B; ++j)
       if (k + j < a.n) {
-        const Sum w = Sum(a.w[k + j]);
+        const double w = a.w[k + j];
 #pragma unroll
         for (int i = 0; i < P; ++i) {
           const Four v = Src::values(s[j][i]);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) acc[i][q] = mad(w, Sum(v.v[q]), acc[i][q]);
+          for (int q = 0; q < 4; ++q) acc[i][q] = fma(w, double(v.v[q]), acc[i][q]);
         }
       }
   }
@@ -448,9 +443,8 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a) {
     for (int i = 0; i < P; ++i)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const double d = own[i].has(uint32_t(q)) ? double(acc[i][q]) : 0.0;
+        const double d = own[i].has(uint32_t(q)) ? acc[i][q] : 0.0;
         squares = fma(d, d, squares);
-        x[i].v[q] = float(acc[i][q]);
       }
     squares = join_lanes<kLanes>(squares, add);
     if constexpr (kWaves > 1) {
@@ -464,11 +458,11 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a) {
   } else {
     // Sums about the row's first element, so that one pass gives the mean and
     // the squares about it: x - x_0 loses nothing in fp64 that matters to x.
-    Sum f = Sum(0);
+    double f = 0.0;
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       if (uint32_t(q) == own[0].lo) f = acc[0][q];
-    double about = double(__shfl(f, 0, kLanes));
+    double about = __shfl(f, 0, kLanes);
     if constexpr (kWaves > 1) {
       if (threadIdx.x == 0) sums[0][2] = about;
       __syncthreads();
@@ -479,7 +473,7 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a) {
     for (int i = 0; i < P; ++i)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const double d = own[i].has(uint32_t(q)) ? double(acc[i][q]) - about : 0.0;
+        const double d = own[i].has(uint32_t(q)) ? acc[i][q] - about : 0.0;
         sum += d;
         squares = fma(d, d, squares);
       }
@@ -504,13 +498,13 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a) {
 #pragma unroll
     for (int i = 0; i < P; ++i)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) x[i].v[q] = float(double(acc[i][q]) - mean);
+      for (int q = 0; q < 4; ++q) acc[i][q] -= mean;
   }
-  const float r = float(inverse_root(var + a.eps));
+  const double r = inverse_root(var + a.eps);
 #pragma unroll
   for (int i = 0; i < P; ++i)
 #pragma unroll
-    for (int q = 0; q < 4; ++q) x[i].v[q] *= r;
+    for (int q = 0; q < 4; ++q) x[i].v[q] = float(acc[i][q] * r);
   if (a.gain || a.shift) {
     uint32_t group = __umulhi(row, a.group_inverse);  // row / rows_per_group, or one less
     if (row - group * a.rows_per_group >= a.rows_per_group) ++group;
@@ -528,21 +522,26 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a) {
         }
       }
     };
-    if (a.gain) {
-      Four g[P];
+    Four g[P], b[P];
+    if (a.gain && a.shift) {
+      row_of(a.gain, g);
+      row_of(a.shift, b);
+#pragma unroll
+      for (int i = 0; i < P; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[i].v[q] = fmaf(x[i].v[q], g[i].v[q], b[i].v[q]);
+    } else if (a.gain) {
       row_of(a.gain, g);
 #pragma unroll
       for (int i = 0; i < P; ++i)
 #pragma unroll
         for (int q = 0; q < 4; ++q) x[i].v[q] *= g[i].v[q];
-    }
-    if (a.shift) {
-      Four g[P];
-      row_of(a.shift, g);
+    } else {
+      row_of(a.shift, b);
 #pragma unroll
       for (int i = 0; i < P; ++i)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) x[i].v[q] += g[i].v[q];
+        for (int q = 0; q < 4; ++q) x[i].v[q] += b[i].v[q];
     }
   }
   const auto highest = [](uint32_t u, uint32_t v) { return max(u, v); };

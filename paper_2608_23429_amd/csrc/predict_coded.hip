@@ -166,7 +166,6 @@ hipError_t launch_ns_no(const Job &j, hipStream_t s) {
   h.scale_super = j.place->scale_super;
   constexpr CodedShape kShape = coded_shape(NS, NO);
   constexpr int R = kShape.runs;
-  // -- shape
   const uint32_t tiles = uint32_t(j.numel / (512 * R));
   const int blocks = j.waves != 0 ? j.waves : coded_blocks(NS, NO, Out::kBytes, j.numel, j.cus);
   hipLaunchKernelGGL((predict_coded_kernel<Fmt, Out, NS, NO, R, kShape.lines>), dim3(tiles),

@@ -27,21 +27,16 @@ def half_step(y, out):
 
 def reference(srcs, w, x_in, kind, gain, shift, eps=EPS):
     """(x, y, bound on y before its last rounding), [rows, dim] fp64.  The bound
-    counts fp32 roundings: x's, h's, the factor's, the products' and the sum's.
-    x's: 16- and 8-bit sources are summed in fp32, each weight rounded, then n
-    products and sums and the residual's addition, so (n + 2) 2^-24 of the sum
-    of magnitudes |x_in| + sum |w s|; h's in fp64, rounded once."""
+    counts fp32 roundings: x's, h's, the factor's, the products' and the sum's."""
     x = np.zeros_like(srcs[0]) if x_in is None else x_in.copy()
-    size = np.abs(x)
     for a, s in zip(w, srcs):
         x = x + a * s
-        size = size + np.abs(a * s)
     rows, dim = x.shape
-    size = (len(srcs) + 2) / 2 * size
+    size = np.abs(x)
     h = x
     if kind == "layer":
         h = x - x.mean(1, keepdims=True)
-        size = size + size.mean(1, keepdims=True)
+        size = size + np.abs(x).mean(1, keepdims=True)
     var = (h * h).mean(1, keepdims=True) + eps
     r = 1.0 / np.sqrt(var)
     g, b = np.ones((rows, dim)), np.zeros((rows, dim))
@@ -121,10 +116,10 @@ def test_add_norm_dims(dim, out):
                                  shift=b, out=DTYPES.get(out, out))
         want_x, want, bound = reference([f64(s) for s in srcs], w, f64(x), kind, f64(gain),
                                         f64(shift))
-        # fp32 sums (n + 2 roundings of the magnitudes), one to the residual's type
+        # one rounding to fp32, one to the residual's type
         off = np.abs(f64(x_out) - want_x)
-        sums = 4 * U * (np.abs(f64(x)) + sum(abs(a) * np.abs(f64(s)) for a, s in zip(w, srcs)))
-        assert (off <= sums + half_step(np.abs(want_x) + sums, x_dtype)).all(), off.max()
+        assert (off <= half_step(want_x, "f32") + half_step(np.abs(want_x) * (1 + U),
+                                                            x_dtype)).all(), off.max()
         check(out, y, want, bound)
         again = cheb.add_norm(dev, w, x_in, x_in, kind=kind, eps=EPS, gain=g, shift=b,
                               out=DTYPES.get(out, out))      # in place
@@ -183,12 +178,24 @@ def test_residual_norm(dim, first, n, dtype, layout, quant):
         x_in, gd = cuda(x, gain)
         x_out, y = cache.residual_norm(w, 1, torch.empty_like(x_in), x_in, dim=dim, first=first,
                                        rows=rows, eps=EPS, gain=gd, out=DTYPES.get(out, out))
-        if dtype == "f32" and quant is None:      # fp64 sums, one rounding
-            assert (np.abs(f64(x_out) - want_x) <= half_step(want_x, "f32") * 1.01).all()
-        else:                                     # fp32 sums
-            sums = (n + 2) * U * (np.abs(f64(x)) + sum(abs(a) * np.abs(s) for a, s in zip(w, srcs)))
-            assert (np.abs(f64(x_out) - want_x) <= sums * 1.01).all()
+        assert (np.abs(f64(x_out) - want_x) <= half_step(want_x, "f32") * 1.01).all()
         check(out, y, want, bound)
+    cache.close()
+
+
+@pytest.mark.parametrize("layout", ["slots", "interleaved"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_residual_is_residual_apply_16(dtype, layout):
+    """x_out is cheb_residual_apply's bit for bit over 16-bit entries too."""
+    numel = 7 * 768
+    cache = cheb.ChebCache(3, DTYPES[dtype], [numel], layout=layout)
+    g = torch.Generator().manual_seed(2)
+    for k in range(3):
+        cache.push(float(k), [torch.randn(numel, generator=g).to(DTYPES[dtype]).cuda()])
+    x = torch.randn(numel, generator=g).cuda()
+    w = [1.7, -3.3, 2.6]
+    x_out, _ = cache.residual_norm(w, 0, torch.empty_like(x), x, dim=768)
+    assert torch.equal(cache.residual_apply(w, [0], torch.empty_like(x), x), x_out)
     cache.close()
 
 
