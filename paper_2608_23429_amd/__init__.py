@@ -395,7 +395,7 @@ class ResidualHistory:
         Rows of ``dim`` from the residual's element ``first`` on: all of it, or
         ``rows`` of them (the image tokens, say); x_in and x_out hold those.
         Other arguments as add_norm's."""
-        w = cheb_precompute_weights(self.history(), [target_t])[0]
+        w = _binding.weights_at(self.cache.handle, target_t)
         x_out, y = self.cache.residual_norm(w, 0, x_out, x_in, dim=dim, first=first, rows=rows,
                                             kind=kind, eps=eps, gain=gain, shift=shift, out=out,
                                             stream=stream)
@@ -545,15 +545,19 @@ class ChebCache:
         if len(segments) != len(self.seg_numel):
             raise ChebError(_binding.CHEB_E_MISMATCH, "segment count differs from the layout")
         dtype, ptrs = self.dtype, []
+        if self.quant is not None:
+            self._check_here(stream)
+            device = self.device.index
         for s, n in zip(segments, self.seg_numel):
             if not (isinstance(s, torch.Tensor) and s.is_cuda and s.dtype is dtype
                     and s.numel() == n and s.is_contiguous()):
                 _check_device_tensor(s, f"segments[{len(ptrs)}]")
                 raise ChebError(_binding.CHEB_E_MISMATCH,
                                 f"segments[{len(ptrs)}] differs from the layout")
+            if self.quant is not None and s.get_device() != device:
+                raise ChebError(_binding.CHEB_E_INVAL, f"segments[{len(ptrs)}] is on {s.device}, "
+                                f"the cache on {self.device}")
             ptrs.append(s.data_ptr())
-        if self.quant is not None:
-            self._check_here(stream, *segments)
         cheb_cache_push(self._h, t, ptrs, _stream_handle(stream))
 
     def begin_push(self) -> torch.Tensor:
@@ -652,7 +656,7 @@ class ChebCache:
         as many as fit or ``rows``; other arguments as add_norm's."""
         if not 0 <= seg < len(self.seg_numel):
             raise ChebError(_binding.CHEB_E_INVAL, f"segment {seg} out of range")
-        w = np.asarray(w, dtype=np.float64).reshape(-1)
+        w = np.asarray(w, dtype=np.float64)
         if w.size != self.n_slots:
             raise ChebError(_binding.CHEB_E_INVAL, f"{w.size} weights for {self.n_slots} entries")
         dim, left = int(dim), self.seg_numel[seg] - first

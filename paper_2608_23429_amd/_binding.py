@@ -407,6 +407,15 @@ def cheb_cache_history(handle, n_slots=CHEB_MAX_SLOTS):
     return _doubles(t, n.value)
 
 
+def weights_at(handle, target) -> np.ndarray:
+    """cheb_precompute_weights' row of the held abscissae at one target."""
+    t, w = _Slots(), _Slots()
+    n = ctypes.c_int32()
+    _check(LIB.cheb_cache_history(handle, t, ctypes.byref(n)))
+    _check(LIB.cheb_precompute_weights(t, n.value, ctypes.byref(ctypes.c_double(target)), 1, w))
+    return _doubles(w, n.value)
+
+
 def cheb_cache_entry(handle, idx) -> int:
     p = ctypes.c_void_p()
     _check(LIB.cheb_cache_entry(handle, int(idx), ctypes.byref(p)))
@@ -546,9 +555,7 @@ def cheb_add_norm(src_ptrs, w, dtype, norm, stream=0):
 
 
 def cheb_residual_norm(handle, w, seg, first, norm, stream=0):
-    w = _f64(w).reshape(-1)
-    _check(LIB.cheb_residual_norm(handle, _dptr(w), int(seg), int(first), ctypes.byref(norm),
-                                  int(stream)))
+    _check(LIB.cheb_residual_norm(handle, _dptr(_f64(w)), seg, first, ctypes.byref(norm), stream))
 
 
 def cheb_get_launch_config():
