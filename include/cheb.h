@@ -607,7 +607,8 @@ enum { CHEB_NORM_RMS = 0, CHEB_NORM_LAYER = 1 };
  *                     y_scale [rows][ceil(dim / 32)].  A group with a NaN or an
  *                     infinity has scale 255 (NaN) and codes 0.
  *   CHEB_OUT_FP8_ROW  one fp32 scale a row, max|y| / 448 (1 for a row of zeros,
- *                     at least 2^-126), codes y / scale rounded to nearest even.
+ *                     at least 2^-126), codes y times the scale's fp32
+ *                     reciprocal, rounded to nearest even.
  *                     y_scale [rows].  A row with a NaN or an infinity has a NaN
  *                     scale and codes 0. */
 enum { CHEB_OUT_MXFP8 = 16, CHEB_OUT_FP8_ROW = 17 };
@@ -660,8 +661,9 @@ CHEB_API int cheb_add_norm(const void *const *src, int32_t n_src, const double *
  * contribution).  Any cache, of either layout and of 8-bit entries too.
  *   w    [n_slots] host fp64, aligned with cheb_cache_history.
  * Requires a full history.  Over plain entries an fp32 x_out equals, bit for bit,
- * cheb_residual_apply's with that segment alone.  Errors: CHEB_E_INVAL (also a range past the tensor),
- * CHEB_E_NOTREADY, CHEB_E_DTYPE, CHEB_E_ALIGN, CHEB_E_NONFINITE, CHEB_E_HIP. */
+ * cheb_residual_apply's with that segment alone.  Errors: CHEB_E_INVAL (also a
+ * range past the tensor), CHEB_E_NOTREADY, CHEB_E_DTYPE, CHEB_E_ALIGN,
+ * CHEB_E_NONFINITE, CHEB_E_HIP. */
 CHEB_API int cheb_residual_norm(cheb_cache *c, const double *w, int32_t seg, int64_t first,
                                 const cheb_norm *norm, void *stream);
 

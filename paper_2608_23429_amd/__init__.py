@@ -278,7 +278,7 @@ def _norm_call(current, device, x_out, x_in, numel, dim, kind, eps, gain, shift,
         groups = of_shift
     if type(out) is str or type(out) is torch.dtype:
         out = norm_output(rows, dim, out, device)
-    if type(out) is tuple:
+    if isinstance(out, (tuple, list)) and len(out) == 2:
         y, scale = out
         _here(scale, "out's scales", current)
         scale_ptr = scale.data_ptr()
@@ -288,14 +288,14 @@ def _norm_call(current, device, x_out, x_in, numel, dim, kind, eps, gain, shift,
                 or (fmt == CHEB_OUT_MXFP8 and scale.dtype is not torch.float8_e8m0fnu)):
             raise ChebError(_binding.CHEB_E_MISMATCH, "out differs from norm_output's")
     else:
-        y, fmt = out, _DTYPES.get(out.dtype)
+        y, fmt = out, _DTYPES.get(getattr(out, "dtype", None))
         if fmt is None:
-            raise ChebError(_binding.CHEB_E_DTYPE, f"unsupported dtype {y.dtype}")
+            raise ChebError(_binding.CHEB_E_DTYPE, "out is of no supported dtype")
     _here(y, "out", current)
     if y.numel() != numel:
         raise ChebError(_binding.CHEB_E_MISMATCH, f"out holds {y.numel()} elements, not {numel}")
     return cheb_norm(rows, dim, eps, in_ptr, out_ptr, gain_ptr, shift_ptr,
-                     rows // groups if groups else 0, y.data_ptr(), scale_ptr, norm, x_dt,
+                     max(rows // groups, 1) if groups else 0, y.data_ptr(), scale_ptr, norm, x_dt,
                      fmt), out
 
 

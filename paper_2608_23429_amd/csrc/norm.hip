@@ -342,12 +342,12 @@ __device__ __forceinline__ void add_rows(double (&sum)[P][4], const Raw (&x0)[P]
 // overflow nor cancel, so y is rounded to fp32 once before its gain and shift:
 // an 8-bit code then flips beside a tie less often than it would by an fp32
 // chain.  (All of it in fp32 for 16- and 8-bit sources: 0 to 9% less time; 16384 x
-// 1152, one bf16 source, layer norm 27.8 us for 29.6.)  Sources carry the non-temporal hint, and so
-// does x_out, which is read a whole block later; x_in may be in a cache still,
-// and y is read next.  Measured on MI355X:
+// 1152, one bf16 source, layer norm: 27.8 us for 29.6.)  Sources carry the
+// non-temporal hint, and so does x_out, which is read a whole block later; x_in
+// may be in a cache still, and y is read next.  Measured on MI355X:
 //   8192 x 1152, 6 bf16 entries into MXFP8: 33.0 us, 6.0 TB/s (39.6 without the
-//   hints); 16384 x 1152, layer norm of 4 fp32 entries: 75.8 us, 6.2 TB/s (88);
-//   5003 x 1155 in fp16, a scale a row: 10.9 us.
+//   hints); 16384 x 1152, layer norm of 4 fp32 entries: 74.5 us, 6.3 TB/s (88);
+//   5003 x 1155 in fp16, a scale a row: 11.1 us.
 template <class Src, int L, int P, int B, int M>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a) {
   constexpr int kThreads = L < 256 ? 256 : L, kWaves = L > 64 ? L / 64 : 1;

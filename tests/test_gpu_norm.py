@@ -259,6 +259,25 @@ def test_rows_that_are_not_finite(dim):
             assert np.isnan(f64(scale)[6, 0]) and (f64(scale)[1] == 2.0 ** -120).all()
 
 
+@pytest.mark.parametrize("dim", [40, 1155])
+def test_no_rows_with_a_gain(dim):
+    empty = torch.empty(0, dim, dtype=torch.bfloat16, device="cuda")
+    gain = torch.ones(dim, device="cuda")
+    for out in (torch.bfloat16, "fp8_row"):
+        _, y = cheb.add_norm([empty], [1.0], None, empty, gain=gain, shift=gain, out=out)
+        assert (y if isinstance(y, torch.Tensor) else y[0]).shape == (0, dim)
+
+
+def test_refusals_of_outputs():
+    x = torch.ones(4, 64, device="cuda")
+    codes, scale = cheb.norm_output(4, 64, "mxfp8")
+    for out in (None, (codes,), codes, (codes, codes), (codes[:3], scale), (codes, scale[:3]),
+                (codes.t(), scale), (codes.cpu(), scale), torch.ones(4, 64), "bf16", torch.int8):
+        with pytest.raises(cheb.ChebError):
+            cheb.add_norm([x], [1.0], out=out)
+    assert cheb.add_norm([x], [1.0], out=[codes, scale])[1][0] is codes
+
+
 def test_no_rows_and_views():
     """No rows; and rows taken from the middle of larger tensors, whose
     neighbours stay as they were."""
