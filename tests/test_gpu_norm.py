@@ -294,3 +294,47 @@ def test_no_rows_and_views():
         assert (t[0] == 7).all() and (t[4] == 7).all() and not (t[1:4] == 7).all()
     assert scale[0] == 9 and scale[4] == 9
     assert torch.equal(dest[1:4], (src.double() + x.double()).float().half())
+
+
+@pytest.mark.parametrize("dim,out", [(1152, "mxfp8"), (1155, "fp8_row")])
+def test_rows_past_32_bits(dim, out):
+    """Element numbers past 2^32: the last rows are what a call on them alone
+    gives, bit for bit, and rows before them what zeros give."""
+    print(f"rows_past_32_bits {dim} {out}", flush=True)
+    rows, last = (1 << 32) // dim + 50, 37
+    src = torch.zeros(rows, dim, dtype=torch.bfloat16, device="cuda")
+    tail = torch.randn(last, dim, generator=torch.Generator().manual_seed(dim)).bfloat16().cuda()
+    src[-last:] = tail
+    codes, scale = cheb.norm_output(rows, dim, out)
+    x = src.clone()
+    cheb.add_norm([src], [1.5], x, x, out=(codes, scale))
+    x_want, (want, want_scale) = cheb.add_norm([tail], [1.5], torch.empty_like(tail), tail, out=out)
+    assert torch.equal(x[-last:], x_want) and not x[:-last].any()
+    assert torch.equal(codes[-last:].view(torch.uint8), want.view(torch.uint8))
+    assert torch.equal(scale[-last:].float(), want_scale.float())
+    assert not codes[:-last].view(torch.uint8).any()
+
+
+@pytest.mark.parametrize("quant", [None, "mxint8", "mxfp8"])
+@pytest.mark.parametrize("layout", ["slots", "interleaved"])
+def test_residual_norm_past_32_bits(layout, quant):
+    """The end of a cached tensor of more than 2^32 elements."""
+    print(f"residual_norm_past_32_bits {layout} {quant}", flush=True)
+    dim, numel = 1152, (1 << 32) + 40 * 1152
+    first = numel - 40 * dim
+    g = torch.Generator().manual_seed(4)
+    parts = [torch.randn(40 * dim, generator=g).bfloat16().cuda() for _ in range(2)]
+    small = cheb.ChebCache(2, torch.bfloat16, [40 * dim], layout=layout, quant=quant)
+    large = cheb.ChebCache(2, torch.bfloat16, [numel], layout=layout, quant=quant)
+    whole = torch.zeros(numel, dtype=torch.bfloat16, device="cuda")
+    for k, p in enumerate(parts):
+        small.push(float(k), [p])
+        whole[first:] = p
+        large.push(float(k), [whole])
+    del whole
+    w = [-1.5, 2.5]
+    want_x, want = small.residual_norm(w, 0, torch.empty(40 * dim, device="cuda"), dim=dim)
+    x, y = large.residual_norm(w, 0, torch.empty(40 * dim, device="cuda"), dim=dim, first=first)
+    assert torch.equal(x, want_x) and torch.equal(y, want)
+    small.close()
+    large.close()
