@@ -60,6 +60,22 @@ def _stream_handle(stream: Optional[torch.cuda.Stream], device: Optional[int] = 
     return int(stream.cuda_stream)
 
 
+def _made_for(stream: Optional[torch.cuda.Stream], device, make):
+    """Buffers that a call makes itself and fills on `stream`.  They come from
+    that stream's pool: a block of the current stream's pool may have been freed
+    with work still queued on it, which `stream` does not wait for.  They are
+    not handed out again before the current stream, whose program goes on with
+    them, is done with them either."""
+    if stream is None:
+        return make()
+    user = torch.cuda.current_stream(device)
+    with torch.cuda.stream(stream):
+        made = make()
+    for t in made if isinstance(made, (tuple, list)) else (made,):
+        t.record_stream(user)
+    return made
+
+
 def _check_device_tensor(t: torch.Tensor, what: str):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ChebError(_binding.CHEB_E_INVAL, f"{what} must be a GPU tensor")
@@ -243,7 +259,7 @@ def _norm_rows(t, what: str, dim: int, rows: int) -> int:
     return n // dim
 
 
-def _norm_call(current, device, x_out, x_in, numel, dim, kind, eps, gain, shift, out):
+def _norm_call(current, device, x_out, x_in, numel, dim, kind, eps, gain, shift, out, stream):
     """The norm's structure and its output's buffers; every tensor it takes is
     checked, and lies on the current device."""
     x_dt = CHEB_F32
@@ -277,7 +293,8 @@ def _norm_call(current, device, x_out, x_in, numel, dim, kind, eps, gain, shift,
             raise ChebError(_binding.CHEB_E_MISMATCH, "gain and shift differ in groups")
         groups = of_shift
     if type(out) is str or type(out) is torch.dtype:
-        out = norm_output(rows, dim, out, device)
+        form = out
+        out = _made_for(stream, device, lambda: norm_output(rows, dim, form, device))
     if isinstance(out, (tuple, list)) and len(out) == 2:
         y, scale = out
         _here(scale, "out's scales", current)
@@ -326,7 +343,7 @@ def add_norm(srcs: Sequence[torch.Tensor], w, x_out: Optional[torch.Tensor] = No
     if dim is None:
         dim = like.shape[-1] if like.dim() else 1
     norm, out = _norm_call(current, like.device, x_out, x_in, numel, dim, kind, eps, gain, shift,
-                           out)
+                           out, stream)
     cheb_add_norm(ptrs, w, cheb_dtype(dtype), norm, _stream_here(stream, current))
     return x_out, out
 
@@ -421,6 +438,10 @@ class ChebCache:
     entries, "mxint8" or "mxfp8": ``push`` then quantises tensors of ``dtype``
     in groups of 32 elements, and predictions, ``read`` and the residual update
     decode them; tensors start on multiples of 4096 elements.
+
+    A call with ``stream`` works there, and the caller orders that stream with
+    others as for any work; an output that the call makes itself may be dropped
+    at any time.
     """
 
     def __init__(self, n_slots: int, dtype: torch.dtype, seg_numel: Sequence[int],
@@ -495,6 +516,9 @@ class ChebCache:
     def new_output(self) -> torch.Tensor:
         return torch.empty(self.slot_numel, dtype=self.dtype, device=self.device)
 
+    def _new_output(self, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+        return _made_for(stream, self.device, self.new_output)
+
     def segment_views(self, flat: torch.Tensor, shapes=None) -> List[torch.Tensor]:
         views = []
         for s, (off, n) in enumerate(zip(self.seg_offset, self.seg_numel)):
@@ -532,7 +556,7 @@ class ChebCache:
              stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """The held entry of age index idx (0 = oldest) as a flat tensor of its
         own, whatever the layout; of 8-bit entries the values of the codes."""
-        out = self.new_output() if out is None else out
+        out = self._new_output(stream) if out is None else out
         self._check_out(out)
         if self.quant is not None:
             self._check_here(stream, out)
@@ -585,7 +609,7 @@ class ChebCache:
 
     def extrapolate(self, w, out: Optional[torch.Tensor] = None,
                     stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-        out = self.new_output() if out is None else out
+        out = self._new_output(stream) if out is None else out
         self._check_out(out)
         if self.quant is not None:
             self._check_here(stream, out)
@@ -595,7 +619,7 @@ class ChebCache:
     def extrapolate_multi(self, w, outs: Optional[Sequence[torch.Tensor]] = None,
                           stream: Optional[torch.cuda.Stream] = None):
         w = np.asarray(w, dtype=np.float64).reshape(-1, self.n_slots)
-        outs = [self.new_output() for _ in range(w.shape[0])] if outs is None else list(outs)
+        outs = [self._new_output(stream) for _ in range(w.shape[0])] if outs is None else list(outs)
         for o in outs:
             self._check_out(o)
         if self.quant is not None:
@@ -607,7 +631,7 @@ class ChebCache:
     def extrapolate_at_multi(self, targets, outs: Optional[Sequence[torch.Tensor]] = None,
                              stream: Optional[torch.cuda.Stream] = None):
         targets = list(targets)
-        outs = [self.new_output() for _ in targets] if outs is None else list(outs)
+        outs = [self._new_output(stream) for _ in targets] if outs is None else list(outs)
         for o in outs:
             self._check_out(o)
         if self.quant is not None:
@@ -619,7 +643,7 @@ class ChebCache:
     def extrapolate_steps(self, table: "ChebTable", first_step: int, n_steps: int = 1,
                           outs: Optional[Sequence[torch.Tensor]] = None,
                           stream: Optional[torch.cuda.Stream] = None):
-        outs = [self.new_output() for _ in range(n_steps)] if outs is None else list(outs)
+        outs = [self._new_output(stream) for _ in range(n_steps)] if outs is None else list(outs)
         for o in outs:
             self._check_out(o)
         if self.quant is not None:
@@ -666,13 +690,13 @@ class ChebCache:
         current = torch.cuda.current_device()
         _here(self.arena, "the cache", current)
         norm, out = _norm_call(current, self.device, x_out, x_in, rows * dim, dim, kind, eps, gain,
-                               shift, out)
+                               shift, out, stream)
         cheb_residual_norm(self._h, w, seg, first, norm, _stream_here(stream, current))
         return x_out, out
 
     def extrapolate_at(self, target_t: float, out: Optional[torch.Tensor] = None,
                        stream: Optional[torch.cuda.Stream] = None):
-        out = self.new_output() if out is None else out
+        out = self._new_output(stream) if out is None else out
         self._check_out(out)
         if self.quant is not None:
             self._check_here(stream, out)
