@@ -312,8 +312,8 @@ CHEB_API int cheb_cache_reset(cheb_cache *c);
  * A group with a NaN or an infinity reads back as NaN, all of it.  A value
  * whose code stands for more than the storage type holds reads back as infinity
  * (fp16: beyond 65023 for MXINT8, 63487 for MXFP8).  Predictions sum in fp32 for
- * bf16 and fp16 caches and in fp64 for fp32 ones; residual updates sum the
- * entries of one tensor in fp32 and tensors in fp64. */
+ * bf16 and fp16 caches and in fp64 for fp32 ones; residual updates sum in fp64
+ * for all of them. */
 enum { CHEB_QUANT_NONE = 0, CHEB_QUANT_MXINT8 = 1, CHEB_QUANT_MXFP8 = 2 };
 
 /* The layout of a history of 8-bit entries: as cheb_cache_layout, but cached
@@ -701,8 +701,9 @@ CHEB_API int cheb_residual_norm(cheb_cache *c, const double *w, int32_t seg, int
  *                taken; -1 leaves it free.  The residual calls reserve LDS in
  *                the same way, up to all of it, under limits of their own;
  *                -1 leaves them only what their sums take (at most 64 KiB a
- *                block), other values do not reach them.  Predictions from
- *                8-bit entries take the cap (or -1) and choose the rest.
+ *                block), other values do not reach them.  From 8-bit entries
+ *                predictions take the cap (or -1) and choose the rest, and
+ *                residual updates reserve no more than their sums take.
  * Default {64, 1, 1, 0, 0}.  On MI355X a bf16 history of 5-6 entries
  * streams at 0.83 (contiguous) to 0.87 (interleaved) of the HBM peak under
  * the chosen cap, against 0.75 with 1024-thread blocks at full occupancy:

@@ -70,11 +70,21 @@ struct Halves {
   __device__ __forceinline__ float operator[](int i) const { return float(h[i >> 1][i & 1]); }
 };
 
+// The same codes as fp64 numbers, for sums of more bits: doubles() builds them
+// from their bits, as fp64 conversions run at a quarter of the rate too.  One
+// counts kDouble of its scale.  A sum of them is held as kSum of its value:
+// weights, below 2^128, go in times kDouble kSum, which keeps products with a
+// scale within fp64's range.
+__device__ __forceinline__ double high_word(uint32_t w) {
+  return __builtin_bit_cast(double, uint64_t(w) << 32);
+}
+
 struct Int8Fmt {
   static constexpr uint32_t kLimitFraction = 0x7e0000u;  // 127/64 = 1.984375
   static constexpr int kLimitExponent = 0;
   static constexpr int kShift = 6;        // a code counts 64ths of the scale
   static constexpr double kUnit = 0x1p-6;
+  static constexpr double kDouble = kUnit, kSum = 1.0;
 
   // The stored byte is the code plus 128.  Adding 1.5 2^23 + 128 rounds to the
   // nearest whole number, ties to even, and leaves it as the low byte of the
@@ -113,6 +123,14 @@ struct Int8Fmt {
                off;
     return q;
   }
+
+  // A byte b eight places up in the high word of 2^12 is the number 4096 + b.
+  __device__ __forceinline__ static void doubles(u32x2 v, double (&q)[8]) {
+    constexpr uint32_t kByte[4] = {0x07060004u, 0x07060104u, 0x07060204u, 0x07060304u};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      q[i] = high_word(__builtin_amdgcn_perm(0x40b00000u, v[i >> 2], kByte[i & 3])) - 4224.0;
+  }
 };
 
 struct E4m3Fmt {
@@ -120,6 +138,7 @@ struct E4m3Fmt {
   static constexpr int kLimitExponent = 8;
   static constexpr int kShift = 0;
   static constexpr double kUnit = 1.0;
+  static constexpr double kDouble = 0x1p1016, kSum = 0x1p-248;
 
   __device__ __forceinline__ static u32x2 encode(const float (&x)[8], const Group &g) {
     float v[8];
@@ -154,6 +173,17 @@ struct E4m3Fmt {
       q.h[i] = __builtin_bit_cast(f16x2, (p & 0x80008000u) | (p >> 1 & 0x3fff3fffu)) * up;
     }
     return q;
+  }
+
+  // The code's exponent and fraction at the end of fp64's exponent are the
+  // number of 2^-1016 its value, fp64's small numbers being e4m3's.  The 2^1016
+  // is left to the weights (0.9 of the time of a product here).
+  __device__ __forceinline__ static void doubles(u32x2 v, double (&q)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int32_t p = int32_t(v[i >> 2] << (24 - 8 * (i & 3)));  // below the code: others' bits
+      q[i] = high_word(uint32_t(p >> 7) & 0x80fe0000u);
+    }
   }
 };
 

@@ -13,7 +13,6 @@
 #include "coded.h"
 #include "coded_shapes.h"
 #include "internal.h"
-#include "shapes.h"
 #include "tiles.h"
 
 namespace cheb {
@@ -125,7 +124,7 @@ struct CodedPart {
 template <int NS>
 struct CodedResArgs {
   const char *codes[NS], *scales[NS];
-  float w[NS];
+  double w[NS];  // times kDouble kSum
   int64_t delta[kCover];  // vectors of 8, from an entry's start to the segment's residual vector 0
   CodedPart part[kMaxResIntervals];
   int32_t n_part;
@@ -135,16 +134,14 @@ struct CodedResArgs {
 };
 
 // A tile is a run of 64 residual vectors of 8.  The W waves of a block share it,
-// each taking every W-th batch of U covering segments.  A segment's entries
-// are summed in fp32 (at most 8 terms), segments in fp64, the waves' sums
-// through LDS.  Bound by HBM reads: 33 bytes for 32 elements of each entry and
-// segment.  FLUX-1024, 6 interleaved entries: 785 us, 6.5 TB/s; without its
-// scales it takes 733, so the lines of scales, 1 in 33, cost 7%: each is read by
-// 8 tiles, which are kept on one XCD for that, with those of the next line (797
-// where every XCD reads its own).  Tried and left: 16 elements to a lane, which
-// halves the load instructions (785; DiT 256 19.1 -> 21.3), entries' lines
-// of a block side by side (788, three-target predictions 3% slower), lines next
-// to their codes (858).
+// each taking every W-th batch of U covering segments.  Weights and sums are
+// fp64, as over plain entries, the waves' sums joined through LDS: x is rounded
+// once, whatever the cache's storage type.  Bound by HBM reads: 33 bytes for 32
+// elements of each entry and segment.  FLUX-1024, 6 interleaved entries: 788 us,
+// 6.5 TB/s (786 with sums in fp32; 56 segments of 1152 tiles, 3 entries: 19.6, 19.1;
+// 859 and 21.1 with codes converted to fp64 instead of built).  The lines of
+// scales, 1 in 33, are read by 8 tiles, which are kept on one XCD for that, with
+// those of the next line (833 and 22.1 where every XCD reads its own).
 template <class Fmt, int NS, int W, int U>
 __global__ __launch_bounds__(64 * W) void residual_coded_kernel(CodedResArgs<NS> a) {
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -158,6 +155,9 @@ __global__ __launch_bounds__(64 * W) void residual_coded_kernel(CodedResArgs<NS>
   const uint32_t live = std::min(part.n_vec - first, kRun);
   const uint32_t l = std::min(lane, live - 1u);  // idle lanes repeat the last vector
   const uint64_t j0 = uint64_t(part.vec_begin) + first;
+  const auto added = [](uint32_t x, double sum) {
+    return __float_as_uint(float(fma(sum, 1.0 / Fmt::kSum, double(__uint_as_float(x)))));
+  };
   double acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = -0.0;  // the sum of nothing: x + -0.0 is x, -0.0 too
@@ -185,18 +185,15 @@ __global__ __launch_bounds__(64 * W) void residual_coded_kernel(CodedResArgs<NS>
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int u = 0; u < N; ++u) {
-      float t[8];
+    for (int u = 0; u < N; ++u)
 #pragma unroll
       for (int k = 0; k < NS; ++k) {
-        const float unit = a.w[k] * __uint_as_float(sc[u][k] << 23);
-        const Halves q = Fmt::decode(v[u][k]);
+        const double unit = a.w[k] * double(__uint_as_float(sc[u][k] << 23));
+        double q[8];
+        Fmt::doubles(v[u][k], q);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) t[e] = fmaf(unit, q[e], k == 0 ? 0.0f : t[e]);
+        for (int e = 0; e < 8; ++e) acc[e] = fma(unit, q[e], acc[e]);
       }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += double(t[e]);
-    }
   };
   int32_t c = int32_t(wave) * U;
   for (; c + U <= part.ncover; c += W * U) take(std::integral_constant<int, U>(), c);
@@ -212,7 +209,7 @@ __global__ __launch_bounds__(64 * W) void residual_coded_kernel(CodedResArgs<NS>
       if (a.x_in) x = *reinterpret_cast<const u32x4 *>(a.x_in + o + 4 * h);
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        r[q] = __float_as_uint(float(double(__uint_as_float(x[q])) + acc[4 * h + q]));
+        r[q] = added(x[q], acc[4 * h + q]);
       *reinterpret_cast<u32x4 *>(a.x_out + o + 4 * h) = r;
     }
   } else {
@@ -229,10 +226,10 @@ __global__ __launch_bounds__(64 * W) void residual_coded_kernel(CodedResArgs<NS>
       if (a.x_in) x = *reinterpret_cast<const u32x4 *>(a.x_in + o);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        double s = double(__uint_as_float(x[q]));
+        double s = sums[0][at + uint32_t(q) * 64u];
 #pragma unroll
-        for (int w = 0; w < W; ++w) s += sums[w][at + uint32_t(q) * 64u];
-        r[q] = __float_as_uint(float(s));
+        for (int w = 1; w < W; ++w) s += sums[w][at + uint32_t(q) * 64u];
+        r[q] = added(x[q], s);
       }
       *reinterpret_cast<u32x4 *>(a.x_out + o) = r;
     }
@@ -249,8 +246,6 @@ struct CodedResJob {
   const float *x_in;
   float *x_out;
   const CodedPlace *place;
-  int cus, lds_per_cu;
-  int waves;  // the launch shape's waves_per_cu: -1 leaves the LDS free
 };
 
 template <class Fmt, int NS>
@@ -260,7 +255,7 @@ hipError_t launch_residual_ns(const CodedResJob &j, hipStream_t s) {
   for (int k = 0; k < NS; ++k) {
     a.codes[k] = j.src[k].codes;
     a.scales[k] = j.src[k].scales;
-    a.w[k] = float(j.w[k] * Fmt::kUnit);
+    a.w[k] = j.w[k] * (Fmt::kDouble * Fmt::kSum);
   }
   memcpy(a.delta, j.delta, sizeof(int64_t) * size_t(j.n_delta));
   a.code_super = uint32_t(j.place->code_super);
@@ -277,16 +272,16 @@ hipError_t launch_residual_ns(const CodedResJob &j, hipStream_t s) {
     ncover = std::max(ncover, int(j.iv[i].ncover));
   }
   constexpr int U = 2;  // segments ahead of their sums
-  const CodedResShape shape = coded_residual_shape(NS, ncover, tiles);
-  const auto launch = [&](auto kernel, int waves, size_t own) {
-    hipLaunchKernelGGL(kernel, dim3(tiles), dim3(64 * waves),
-                       residual_lds(j.lds_per_cu, shape.blocks_per_cu, own, j.waves), s, a);
+  const auto launch = [&](auto kernel, int waves) {
+    hipLaunchKernelGGL(kernel, dim3(tiles), dim3(64 * waves), 0, s, a);
     return hipGetLastError();
   };
-  if (shape.waves == 1) return launch(residual_coded_kernel<Fmt, NS, 1, U>, 1, 0);
-  if (shape.waves == 2) return launch(residual_coded_kernel<Fmt, NS, 2, U>, 2, 2 * 4096);
-  if (shape.waves == 4) return launch(residual_coded_kernel<Fmt, NS, 4, U>, 4, 4 * 4096);
-  return launch(residual_coded_kernel<Fmt, NS, 8, U>, 8, 8 * 4096);
+  switch (coded_residual_waves(NS, ncover, tiles)) {
+    case 1: return launch(residual_coded_kernel<Fmt, NS, 1, U>, 1);
+    case 2: return launch(residual_coded_kernel<Fmt, NS, 2, U>, 2);
+    case 4: return launch(residual_coded_kernel<Fmt, NS, 4, U>, 4);
+    default: return launch(residual_coded_kernel<Fmt, NS, 8, U>, 8);
+  }
 }
 
 template <class Fmt>
@@ -337,10 +332,7 @@ int launch_residual_coded(int quant, int n, const CodedEntry *src, const double 
                           const int64_t *delta, int n_delta, const ResidualInterval *iv, int n_iv,
                           const float *x_in, float *x_out, const CodedPlace &place,
                           hipStream_t stream) {
-  CodedResJob j{src, w, delta, n_delta, iv, n_iv, x_in, x_out, &place, 0, 0,
-                launch_shape().waves_per_cu};
-  int rc = device_info(&j.cus, &j.lds_per_cu);
-  if (rc != CHEB_OK) return rc;
+  const CodedResJob j{src, w, delta, n_delta, iv, n_iv, x_in, x_out, &place};
   const hipError_t e = quant == CHEB_QUANT_MXINT8 ? launch_residual_fmt<Int8Fmt>(n, j, stream)
                                                   : launch_residual_fmt<E4m3Fmt>(n, j, stream);
   if (e != hipSuccess) return fail(CHEB_E_HIP, "residual launch failed: %s", hipGetErrorString(e));

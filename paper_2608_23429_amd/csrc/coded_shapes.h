@@ -42,23 +42,19 @@ inline int coded_blocks(int ns, int no, int out_bytes, int64_t numel, int cus) {
 
 // The waves that share a residual tile; each loads two segments ahead of its
 // sums.  One segment is one wave's; a second wave pays from two on (2 segments
-// of one entry, 36.9K tiles: 33.3 us, 37.0 with one), four where there is much to
-// read (24 segments of 2 entries, 1152 tiles: 7.9 us, 8.5 with two; 8 segments of
-// one entry: 50.9 with two, 57 with four), and eight for many segments of three
-// entries or more (DiT-XL/2 256, 56 segments of 3 entries: 19.1, 20.3 with four).
-// Five entries or more fill the queues by themselves: 16 waves a compute unit
-// (FLUX-1024: 785, 797 without a limit).
-struct CodedResShape {
-  int waves;
-  int blocks_per_cu;  // 0: no limit
-};
-inline CodedResShape coded_residual_shape(int ns, int ncover, uint32_t tiles) {
+// of one entry, 36.9K tiles: 31.8 us, 37.7 with one; but 8 of them 49.7, 55.0 with
+// four), four where there is much to read (24 segments of 2 entries, 1152 tiles:
+// 8.1 us, 9.4 with two; FLUX-1024, 6 entries: 787, 789 with eight; 10 segments of 6
+// entries, 18.4K tiles: 100.6, 104.5 with two, 113.2 with eight), and eight for
+// many segments where the tiles are few (56 segments of 6 entries, 1152 tiles:
+// 34.7, 36.5 with four; of 3 entries, 2304 tiles: 34.8, 36.7; from 4608 tiles on
+// alike).  A limit on the blocks that share a compute unit gains under 1%.
+inline int coded_residual_waves(int ns, int ncover, uint32_t tiles) {
   // HIP refuses a grid of 2^32 threads, which 8 waves a tile reach at 2^23.
-  if (tiles >= uint32_t(1) << 23) return {1, 0};
-  if (ncover <= 1) return {1, 0};
-  if (ncover <= 4 || (ns == 1 && ncover <= 28)) return {2, 0};
-  if (ns >= 3 && ncover >= 24) return {8, ns >= 5 ? 2 : 0};
-  return {4, ns >= 5 ? 4 : 0};
+  if (tiles >= uint32_t(1) << 23 || ncover <= 1) return 1;
+  if (ncover <= 4 || (ns == 1 && ncover <= 28)) return 2;
+  if (ncover >= 24 && ns >= 2 && tiles <= 4096) return 8;
+  return 4;
 }
 
 }  // namespace cheb
