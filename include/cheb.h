@@ -311,7 +311,8 @@ CHEB_API int cheb_cache_reset(cheb_cache *c);
  *                      beside a large one.
  * A group with a NaN or an infinity reads back as NaN, all of it.  A value
  * whose code stands for more than the storage type holds reads back as infinity
- * (fp16: beyond 65023 for MXINT8, 63487 for MXFP8).  Predictions sum in fp32 for
+ * (fp16: beyond 65023 for MXINT8, 63487 for MXFP8); residual updates and norms
+ * take it for what the code stands for.  Predictions sum in fp32 for
  * bf16 and fp16 caches and in fp64 for fp32 ones; residual updates sum in fp64
  * for all of them. */
 enum { CHEB_QUANT_NONE = 0, CHEB_QUANT_MXINT8 = 1, CHEB_QUANT_MXFP8 = 2 };
@@ -659,8 +660,9 @@ CHEB_API int cheb_add_norm(const void *const *src, int32_t n_src, const double *
  * cached tensor `seg` of every held entry, oldest to newest (the predicted
  * output of that module, or with a collapsed history the block stack's whole
  * contribution).  Any cache, of either layout and of 8-bit entries too.
- *   w    [n_slots] host fp64, aligned with cheb_cache_history.
- * Requires a full history.  Over plain entries an fp32 x_out equals, bit for bit,
+ *   w    [n_slots] host fp64, aligned with cheb_cache_history; over 8-bit
+ *        entries of fp32's range.
+ * Requires a full history.  An fp32 x_out equals, bit for bit,
  * cheb_residual_apply's with that segment alone.  Errors: CHEB_E_INVAL (also a
  * range past the tensor), CHEB_E_NOTREADY, CHEB_E_DTYPE, CHEB_E_ALIGN,
  * CHEB_E_NONFINITE, CHEB_E_HIP. */

@@ -2,6 +2,7 @@
 // sources of cheb_add_norm and cheb_residual_norm.  (Paper, Section 3.1, block
 // equation: module outputs are added to the residual stream; Section 3.3: on a
 // skipped step their predictions are.)
+#include <float.h>
 #include <math.h>
 
 #include "cache.h"
@@ -131,8 +132,11 @@ int cheb_residual_norm(cheb_cache *c, const double *w, int32_t seg, int64_t firs
   if (c->push_open) return fail(CHEB_E_NOTREADY, "a fused push is open");
   if (c->count < c->n_slots)
     return fail(CHEB_E_NOTREADY, "history holds %d of %d entries", c->count, c->n_slots);
-  for (int32_t k = 0; k < c->n_slots; ++k)
+  for (int32_t k = 0; k < c->n_slots; ++k) {
     if (!isfinite(w[k])) return fail(CHEB_E_NONFINITE, "w[%d] is not finite", k);
+    if (c->coded && fabs(w[k]) > double(FLT_MAX))
+      return fail(CHEB_E_NONFINITE, "weight %d (%.17g) overflows fp32", k, w[k]);
+  }
   if (norm->rows == 0) return ok();
   const Span arena = span(c->arena, int64_t(c->arena_bytes));
   rc = check_buffers(*norm, &arena, 1);

@@ -131,6 +131,16 @@ __device__ __forceinline__ void store_four(char *p, const Four &x, const Own &ow
   }
 }
 
+// How a row's elements fall into fours.
+//   kEven  dim is a multiple of four (and so is the sources' first element,
+//          where fours must not cross a chunk or a group): every four is the
+//          row's own or none of it is.
+//   kOdd   contiguous sources of any dim: a row's last four reaches into the next
+//          row, and in the last rows, which have none, starts earlier instead.
+//   kSplit sources whose fours may cross a chunk or a group, or of fewer than
+//          four elements in all: element by element.
+enum { kEven, kOdd, kSplit };
+
 // Where a row of the sources starts: `rb` bytes (scales: `rs`) from an entry's
 // base, `in` elements into a chunk (0: contiguous sources).
 struct RowAt {
@@ -146,6 +156,7 @@ struct PlainSrc {
   using At = uint32_t;                                      // bytes from the row's base
   static constexpr uint32_t kLg = DT == CHEB_F32 ? 13 : 14;  // elements of a chunk
   static constexpr bool kAnyPlace = true;                    // fours may start at any element
+  static constexpr double kSum = 1.0;                        // sums are held as that of their value
 
   __device__ __forceinline__ static RowAt row(const NormArgs &a, uint64_t e) {
     if (!a.chunked) return {e * Type::kSize, 0u, 0u};
@@ -169,10 +180,17 @@ struct PlainSrc {
                             at(a, r, el + uint32_t(q)));
     return h;
   }
-  __device__ __forceinline__ static Four values(const Held &h) { return Type::values(h); }
+  template <int M>
+  __device__ __forceinline__ static void add(double (&sum)[4], double w, const Held &h) {
+    const Four x = Type::values(h);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sum[q] = fma(w, double(x.v[q]), sum[q]);
+  }
 };
 
-// 8-bit entries: four codes and, a byte each, their scales.
+// 8-bit entries: four codes and their scale (kSplit: scales, a byte each).
+// Codes are taken as fp64 numbers, so that one of 2^128 or more, beside fp32's
+// largest values, counts; weights come times kDouble kSum.
 template <class Fmt>
 struct CodedSrc {
   struct Held {
@@ -182,6 +200,7 @@ struct CodedSrc {
     uint32_t code, scale;
   };
   static constexpr bool kAnyPlace = false;
+  static constexpr double kSum = Fmt::kSum;
 
   __device__ __forceinline__ static RowAt row(const NormArgs &a, uint64_t e) {
     return {(e >> kCodedChunkLg) * a.super, (e >> kCodedChunkLg) * a.scale_super,
@@ -196,8 +215,7 @@ struct CodedSrc {
   __device__ __forceinline__ static Held four(const NormArgs &a, int k, const RowAt &r, At at) {
     return {__builtin_nontemporal_load(
                 reinterpret_cast<const code4_any *>(a.base[k] + r.rb + at.code)),
-            uint32_t(*reinterpret_cast<const uint8_t *>(a.scales[k] + r.rs + at.scale)) *
-                0x01010101u};
+            uint32_t(*reinterpret_cast<const uint8_t *>(a.scales[k] + r.rs + at.scale))};
   }
   __device__ __forceinline__ static Held some(const NormArgs &a, int k, const RowAt &r,
                                               uint32_t el, const Own &own) {
@@ -213,13 +231,17 @@ struct CodedSrc {
       }
     return h;
   }
-  __device__ __forceinline__ static Four values(const Held &h) {
-    const Halves c = Fmt::decode(u32x2{h.codes, 0u});
-    Four x;
+  template <int M>
+  __device__ __forceinline__ static void add(double (&sum)[4], double w, const Held &h) {
+    double c[8];
+    Fmt::doubles(u32x2{h.codes, 0u}, c);
+    double unit = w * double(__uint_as_float(h.scales << 23));
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      x.v[q] = c[q] * (__uint_as_float((h.scales >> (8 * q) & 255u) << 23) * float(Fmt::kUnit));
-    return x;
+    for (int q = 0; q < 4; ++q) {
+      if constexpr (M == kSplit)
+        unit = w * double(__uint_as_float((h.scales >> (8 * q) & 255u) << 23));
+      sum[q] = fma(unit, c[q], sum[q]);
+    }
   }
 };
 
@@ -279,16 +301,6 @@ __device__ __forceinline__ double inverse_root(double v) {
   return s == s ? s : r;  // of 0 and infinity: the first value
 }
 
-// How a row's elements fall into fours.
-//   kEven  dim is a multiple of four (and so is the sources' first element,
-//          where fours must not cross a chunk or a group): every four is the
-//          row's own or none of it is.
-//   kOdd   contiguous sources of any dim: a row's last four reaches into the next
-//          row, and in the last rows, which have none, starts earlier instead.
-//   kSplit sources whose fours may cross a chunk or a group, or of fewer than
-//          four elements in all: element by element.
-enum { kEven, kOdd, kSplit };
-
 template <int DT, int L, int P, int M>
 __device__ __forceinline__ void load_x(Raw (&x)[P], const char *p, const uint32_t (&el)[P],
                                        const Own (&own)[P]) {
@@ -316,10 +328,10 @@ __device__ __forceinline__ void store_rows(void *to, uint64_t r0, const Four (&x
       store_four<DT, M != kEven, kStream>(p + int64_t(int32_t(el[i])) * Stored<DT>::kSize, x[i], own[i]);
 }
 
-// sum = x_in + the sources' sum, kept where that is asked for.
+// sum = x_in + `unit` times the sources' sum, kept where that is asked for.
 template <int DT, int P, int M>
-__device__ __forceinline__ void add_rows(double (&sum)[P][4], const Raw (&x0)[P], void *to,
-                                         uint64_t r0, const uint32_t (&el)[P],
+__device__ __forceinline__ void add_rows(double (&sum)[P][4], double unit, const Raw (&x0)[P],
+                                         void *to, uint64_t r0, const uint32_t (&el)[P],
                                          const Own (&own)[P]) {
   Four x[P];
 #pragma unroll
@@ -327,7 +339,7 @@ __device__ __forceinline__ void add_rows(double (&sum)[P][4], const Raw (&x0)[P]
     x[i] = Stored<DT>::values(x0[i]);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      sum[i][q] = double(x[i].v[q]) + sum[i][q];
+      sum[i][q] = fma(sum[i][q], unit, double(x[i].v[q]));
       x[i].v[q] = float(sum[i][q]);
     }
   }
@@ -423,16 +435,12 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a) {
       if (k + j < a.n) {
         const double w = a.w[k + j];
 #pragma unroll
-        for (int i = 0; i < P; ++i) {
-          const Four v = Src::values(s[j][i]);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) acc[i][q] = fma(w, double(v.v[q]), acc[i][q]);
-        }
+        for (int i = 0; i < P; ++i) Src::template add<M>(acc[i], w, s[j][i]);
       }
   }
-  if (a.x_dtype == CHEB_F32) add_rows<CHEB_F32, P, M>(acc, x0, a.x_out, r0, el, own);
-  else if (a.x_dtype == CHEB_BF16) add_rows<CHEB_BF16, P, M>(acc, x0, a.x_out, r0, el, own);
-  else add_rows<CHEB_F16, P, M>(acc, x0, a.x_out, r0, el, own);
+  if (a.x_dtype == CHEB_F32) add_rows<CHEB_F32, P, M>(acc, 1.0 / Src::kSum, x0, a.x_out, r0, el, own);
+  else if (a.x_dtype == CHEB_BF16) add_rows<CHEB_BF16, P, M>(acc, 1.0 / Src::kSum, x0, a.x_out, r0, el, own);
+  else add_rows<CHEB_F16, P, M>(acc, 1.0 / Src::kSum, x0, a.x_out, r0, el, own);
   Four x[P];
   constexpr int kLanes = L < 64 ? L : 64;
   const auto add = [](double u, double v) { return u + v; };
@@ -660,11 +668,14 @@ hipError_t launch_src(const NormArgs &a, hipStream_t s) {
 int launch_norm(const NormSources &from, const cheb_norm &n, hipStream_t stream) {
   NormArgs a;
   memset(&a, 0, sizeof a);
+  const double unit = from.quant == CHEB_QUANT_MXINT8  ? Int8Fmt::kDouble * Int8Fmt::kSum
+                      : from.quant == CHEB_QUANT_MXFP8 ? E4m3Fmt::kDouble * E4m3Fmt::kSum
+                                                       : 1.0;
   for (int k = 0; k < from.n; ++k) {
     const bool coded = from.quant != CHEB_QUANT_NONE;
     a.base[k] = reinterpret_cast<uint64_t>(coded ? from.src[k].codes : from.base[k]);
     a.scales[k] = coded ? reinterpret_cast<uint64_t>(from.src[k].scales) : 0u;
-    a.w[k] = from.w[k];
+    a.w[k] = from.w[k] * unit;
   }
   a.first = uint64_t(from.first);
   a.n = from.n;

@@ -136,3 +136,32 @@ def test_residual_of_large_values(dtype, quant):
             assert (np.abs(out - want) <= np.abs(want) * 2.0 ** -24 + off)[fine].all()
             np.testing.assert_array_equal(out[~fine], rounded[~fine])
     cache.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_residual_of_the_largest_value(dtype):
+    """MXFP8 rounds fp32's largest value to 2^128, which every call but a read
+    takes for what it is."""
+    x = torch.zeros(64)
+    x[5], x[9] = torch.finfo(DTYPES[dtype]).max, -1.5e38
+    cache, held = ring([[x.to(DTYPES[dtype])]], dtype, "mxfp8")
+    assert held[0, 5] == 2.0 ** 128
+    r = torch.linspace(-1e37, 1e37, 64).cuda()
+    want = (f64(r) + 0.25 * held[0, :64]).astype(np.float32)   # one rounding: exact in fp64
+    for out in (cache.residual_apply([0.25], [0], torch.empty_like(r), r),
+                cache.residual_norm([0.25], 0, torch.empty_like(r), r, dim=64)[0]):
+        np.testing.assert_array_equal(f64(out), want.astype(np.float64))
+    cache.close()
+
+
+@pytest.mark.parametrize("quant", QUANTS)
+def test_weights_past_fp32_refused(quant):
+    cache, _ = ring([tensors([64], "f32", k) for k in range(2)], "f32", quant)
+    x = torch.zeros(64, device="cuda")
+    for call in (lambda w: cache.residual_apply(w, [0], x),
+                 lambda w: cache.residual_norm(w, 0, dim=64)):
+        call([3e38, -3e38])
+        with pytest.raises(cheb.ChebError) as e:
+            call([1.0, 4e38])
+        assert e.value.name == "CHEB_E_NONFINITE"
+    cache.close()
