@@ -32,7 +32,8 @@ struct NormArgs {
 };
 
 // Four elements at any address aligned to one: a load or store of that many
-// bytes takes any alignment.
+// bytes takes any alignment.  (The types lose theirs as template arguments, so
+// they are named where memory is read or written.)
 typedef u32x2 __attribute__((aligned(2))) half4_any;
 typedef u32x4 __attribute__((aligned(4))) float4_any;
 typedef uint32_t __attribute__((aligned(1))) code4_any;
@@ -57,9 +58,13 @@ struct Stored {
   // kStream: read once, with the non-temporal hint.
   template <bool kStream>
   __device__ __forceinline__ static Raw four(const char *p) {
-    using V = std::conditional_t<DT == CHEB_F32, float4_any, half4_any>;
-    if constexpr (kStream) return raw_of(__builtin_nontemporal_load(reinterpret_cast<const V *>(p)));
-    else return raw_of(*reinterpret_cast<const V *>(p));
+    if constexpr (DT == CHEB_F32) {
+      const float4_any *v = reinterpret_cast<const float4_any *>(p);
+      return raw_of(kStream ? __builtin_nontemporal_load(v) : *v);
+    } else {
+      const half4_any *v = reinterpret_cast<const half4_any *>(p);
+      return raw_of(kStream ? __builtin_nontemporal_load(v) : *v);
+    }
   }
   // Element q of the four.
   __device__ __forceinline__ static void one(Raw &r, int q, const char *p) {
@@ -90,8 +95,15 @@ struct Own {
   __device__ __forceinline__ bool all() const { return lo == 0 && hi == 4; }
 };
 
-template <bool kStream, class T, class V>
-__device__ __forceinline__ void put(T *p, V v) {
+template <bool kStream>
+__device__ __forceinline__ void put(char *to, u32x4 v) {
+  float4_any *p = reinterpret_cast<float4_any *>(to);
+  if constexpr (kStream) __builtin_nontemporal_store(v, p);
+  else *p = v;
+}
+template <bool kStream>
+__device__ __forceinline__ void put(char *to, u32x2 v) {
+  half4_any *p = reinterpret_cast<half4_any *>(to);
   if constexpr (kStream) __builtin_nontemporal_store(v, p);
   else *p = v;
 }
@@ -104,7 +116,7 @@ __device__ __forceinline__ void store_four(char *p, const Four &x, const Own &ow
       u32x4 t;
 #pragma unroll
       for (int q = 0; q < 4; ++q) t[q] = __float_as_uint(x.v[q]);
-      put<kStream>(reinterpret_cast<float4_any *>(p), t);
+      put<kStream>(p, t);
     } else {
 #pragma unroll
       for (int q = 0; q < 4; ++q)
@@ -121,7 +133,7 @@ __device__ __forceinline__ void store_four(char *p, const Four &x, const Own &ow
         t[h] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
     }
     if (!kSome || own.all()) {
-      put<kStream>(reinterpret_cast<half4_any *>(p), u32x2{t[0], t[1]});
+      put<kStream>(p, u32x2{t[0], t[1]});
     } else {
 #pragma unroll
       for (int q = 0; q < 4; ++q)
