@@ -84,6 +84,7 @@ struct Int8Fmt {
   static constexpr int kLimitExponent = 0;
   static constexpr int kShift = 6;        // a code counts 64ths of the scale
   static constexpr double kUnit = 0x1p-6;
+  static constexpr int kMostScale = 127;  // 2^127
   static constexpr double kDouble = kUnit, kSum = 1.0;
 
   // The stored byte is the code plus 128.  Adding 1.5 2^23 + 128 rounds to the
@@ -138,6 +139,7 @@ struct E4m3Fmt {
   static constexpr int kLimitExponent = 8;
   static constexpr int kShift = 0;
   static constexpr double kUnit = 1.0;
+  static constexpr int kMostScale = 120;
   static constexpr double kDouble = 0x1p1016, kSum = 0x1p-248;
 
   __device__ __forceinline__ static u32x2 encode(const float (&x)[8], const Group &g) {

@@ -2,10 +2,11 @@
 // application equation): out_m = sum_k w_mk value_k over every element.
 #include <hip/hip_runtime.h>
 
+#include <math.h>
 #include <stdint.h>
-#include <string.h>
 
 #include <algorithm>
+#include <limits>
 #include <type_traits>
 
 #include "coded.h"
@@ -20,9 +21,23 @@ template <int NS, int NO, typename W>
 struct CodedHist {
   const char *codes[NS], *scales[NS];
   void *o[NO];
-  W w[NO][NS];
+  W w[NO][NS];  // times what a code counts of its scale, over `back`
+  W back;
   uint64_t code_super, scale_super;
 };
+
+// A power of two, 1 for weights of ordinary size, that takes the largest weight
+// to where its products with a scale, up to 2^120 for e4m3 and 2^127 for int8,
+// stay in the sums' range: else a zero code beside a large one would give NaN,
+// and sums that are in range infinity.
+template <class Fmt, class W>
+W back_of(const double *w, int n) {
+  double most = 0.0;
+  for (int k = 0; k < n; ++k) most = std::max(most, fabs(w[k]));
+  const int room = std::numeric_limits<W>::max_exponent - Fmt::kMostScale;
+  if (most * Fmt::kUnit < ldexp(1.0, room)) return W(1);
+  return W(ldexp(1.0, ilogb(most * Fmt::kUnit) + 1 - room));
+}
 
 __device__ __forceinline__ float mad(float a, float b, float c) { return fmaf(a, b, c); }
 __device__ __forceinline__ double mad(double a, double b, double c) { return fma(a, b, c); }
@@ -134,6 +149,12 @@ __global__ __launch_bounds__(64) void predict_coded_kernel(
           acc[m][e] = mad(unit, W(q[e]), k == 0 ? W(0) : acc[m][e]);
       }
     }
+    if (std::is_same_v<W, double> || h.back != W(1)) {  // fp64: cheaper than the branch
+#pragma unroll
+      for (int m = 0; m < NO; ++m)
+#pragma unroll
+        for (int e = 0; e < int(V); ++e) acc[m][e] *= h.back;
+    }
 #pragma unroll
     for (int m = 0; m < NO; ++m)
       Out::store(h.o[m], e0 + uint64_t(r) * (64u * V), acc[m]);
@@ -158,9 +179,11 @@ hipError_t launch_ns_no(const Job &j, hipStream_t s) {
     h.codes[k] = j.src[k].codes;
     h.scales[k] = j.src[k].scales;
   }
+  h.back = back_of<Fmt, W>(j.w, NO * NS);
   for (int m = 0; m < NO; ++m) {
     h.o[m] = j.out[m];
-    for (int k = 0; k < NS; ++k) h.w[m][k] = W(j.w[m * NS + k] * Fmt::kUnit);
+    for (int k = 0; k < NS; ++k)
+      h.w[m][k] = W(j.w[m * NS + k] * Fmt::kUnit / double(h.back));
   }
   h.code_super = j.place->code_super;
   h.scale_super = j.place->scale_super;

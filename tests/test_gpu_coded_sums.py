@@ -165,3 +165,42 @@ def test_weights_past_fp32_refused(quant):
             call([1.0, 4e38])
         assert e.value.name == "CHEB_E_NONFINITE"
     cache.close()
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("quant", QUANTS)
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_predict_of_large_values(dtype, quant, layout):
+    """Zeros and small values beside ones near the largest, with weights whose
+    product with the group's scale leaves fp32's range: an element whose own
+    terms are in range is right.  The bound is that of any prediction: weights
+    rounded, n products and sums, and half a step of the output's type."""
+    print(f"predict large {dtype} {quant} {layout}", flush=True)
+    cache, held = ring(large(dtype), dtype, quant, layout)
+    held = held[:, :96]
+    top = float(torch.finfo(DTYPES[dtype]).max)
+    tiny, rel = {"bf16": (2.0 ** -134, 2.0 ** -8), "f16": (2.0 ** -25, 2.0 ** -11),
+                 "f32": (2.0 ** -150, 2.0 ** -24)}[dtype]
+    rows = np.array([[2.0, -1.0], [1024.0, -1023.5], [3.0e5, -2.0e5], [1e-3, 0.5], [0.0, 1.0]])
+    outs = [f64(cache.extrapolate(w)) for w in rows]
+    outs += [f64(o) for o in cache.extrapolate_multi(rows[:4])]
+    for w, out in zip(np.concatenate([rows, rows[:4]]), outs):
+        want, size = w @ held, np.abs(w) @ np.abs(held)
+        fine = size < top * 0.99
+        assert fine.sum() >= 80
+        off = (len(w) + 2) * 2.0 ** (-53 if dtype == "f32" else -24) * size
+        err = np.abs(out[:96] - want)
+        assert (err <= off + np.maximum(np.abs(want) * rel, tiny) * 1.01)[fine].all()
+        assert (out[96:] == 0).all()
+    cache.close()
+
+
+def test_predict_of_weights_past_fp32():
+    """An fp32 cache's weights are fp64 of any size: terms that cancel, and
+    zeros beside one that no fp64 number holds."""
+    a, b = torch.zeros(64), torch.zeros(64)
+    a[0], b[0], a[40] = 2.0 ** -100, 2.0 ** -100, 2.0 ** 100
+    cache, _ = ring([[a], [b]], "f32", "mxfp8")
+    out = f64(cache.extrapolate([2.0 ** 1000, -2.0 ** 1000]))[:64]
+    assert out[40] == np.inf and not np.delete(out, 40).any()
+    cache.close()
