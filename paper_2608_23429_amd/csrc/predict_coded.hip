@@ -33,7 +33,7 @@ struct CodedHist {
 template <class Fmt, class W>
 W back_of(const double *w, int n) {
   double most = 0.0;
-  for (int k = 0; k < n; ++k) most = std::max(most, fabs(w[k]));
+  for (int k = 0; k < n; ++k) most = std::max(most, fabs(double(W(w[k]))));
   const int room = std::numeric_limits<W>::max_exponent - Fmt::kMostScale;
   if (most * Fmt::kUnit < ldexp(1.0, room)) return W(1);
   return W(ldexp(1.0, ilogb(most * Fmt::kUnit) + 1 - room));

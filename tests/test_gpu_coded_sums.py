@@ -204,3 +204,15 @@ def test_predict_of_weights_past_fp32():
     out = f64(cache.extrapolate([2.0 ** 1000, -2.0 ** 1000]))[:64]
     assert out[40] == np.inf and not np.delete(out, 40).any()
     cache.close()
+
+
+@pytest.mark.parametrize("quant,limit", [("mxint8", 2.0 ** 7), ("mxfp8", 2.0 ** 8)])
+def test_predict_of_weights_at_the_limit(quant, limit):
+    """Weights that fp32 rounds up to where they are divided."""
+    x = torch.zeros(64)
+    x[3], x[40] = torch.finfo(torch.bfloat16).max, 1.0
+    cache, _ = ring([[x.bfloat16()]], "bf16", quant)
+    for w in (limit * (1 - 2.0 ** -30), limit, limit * (1 - 2.0 ** -24)):
+        out = f64(cache.extrapolate([w]))[:64]
+        assert out[3] == np.inf and out[40] == limit and not np.delete(out, [3, 40]).any()
+    cache.close()
