@@ -608,8 +608,8 @@ enum { CHEB_NORM_RMS = 0, CHEB_NORM_LAYER = 1 };
  *                     y_scale [rows][ceil(dim / 32)].  A group with a NaN or an
  *                     infinity has scale 255 (NaN) and codes 0.
  *   CHEB_OUT_FP8_ROW  one fp32 scale a row, max|y| / 448 (1 for a row of zeros,
- *                     at least 2^-126), codes y times the scale's fp32
- *                     reciprocal, rounded to nearest even.
+ *                     at least 2^-126), codes the fp32 quotient y / scale,
+ *                     rounded to nearest even.
  *                     y_scale [rows].  A row with a NaN or an infinity has a NaN
  *                     scale and codes 0. */
 enum { CHEB_OUT_MXFP8 = 16, CHEB_OUT_FP8_ROW = 17 };

@@ -282,16 +282,19 @@ __device__ __forceinline__ T join_lanes(T v, Join join) {
   return v;
 }
 
-// Codes of y times `factor` (0: codes 0, whatever y holds).
-template <bool kSome>
-__device__ __forceinline__ void store_codes(char *p, const Four &y, float factor,
+// Codes of y times `factor` (0: codes 0, whatever y holds): exact for a power of
+// two, in fp64 for others.  y times the fp64 reciprocal of an fp32 scale, rounded
+// to fp32, is the fp32 quotient: no quotient of two such numbers is within 2^-49
+// of its size of the middle between two more, and the product is off by 2^-52.
+template <bool kSome, class Factor>
+__device__ __forceinline__ void store_codes(char *p, const Four &y, Factor factor,
                                             const Own &own) {
   float v[4];
 #pragma unroll
-  for (int q = 0; q < 4; ++q) v[q] = y.v[q] * factor;
-  if (__builtin_expect(__ballot(factor == 0.0f) != 0ull, 0)) {
+  for (int q = 0; q < 4; ++q) v[q] = float(Factor(y.v[q]) * factor);
+  if (__builtin_expect(__ballot(factor == Factor(0)) != 0ull, 0)) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = factor == 0.0f ? 0.0f : v[q];
+    for (int q = 0; q < 4; ++q) v[q] = factor == Factor(0) ? 0.0f : v[q];
   }
   int c = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
   c = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], c, true);
@@ -596,13 +599,14 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a) {
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) bits = max(bits, tops[w]);
     }
-    float scale = 1.0f, factor = 1.0f;
+    float scale = 1.0f;
+    double factor = 1.0;
     if (bits >= 0x7f800000u) {
       scale = __uint_as_float(0x7fc00000u);
-      factor = 0.0f;
+      factor = 0.0;
     } else if (bits != 0u) {
       scale = fmaxf(__uint_as_float(bits) / 448.0f, 0x1p-126f);
-      factor = 1.0f / scale;
+      factor = 1.0 / double(scale);
     }
     if (t == 0) static_cast<float *>(a.y_scale)[row] = scale;
 #pragma unroll
