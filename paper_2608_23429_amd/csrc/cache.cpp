@@ -92,8 +92,6 @@ int extrapolate_newest(cheb_cache *c, int32_t used, const double *w, int32_t n_o
     return fail(CHEB_E_NOTREADY, "history holds %d entries, %d needed", c->count, used);
   if (n_out < 1 || n_out > CHEB_MAX_OUTPUTS)
     return fail(CHEB_E_INVAL, "n_out %d outside 1..%d", n_out, CHEB_MAX_OUTPUTS);
-  const void *src[CHEB_MAX_SLOTS];
-  for (int32_t j = 0; j < used; ++j) src[j] = c->slot_ptr(c->slot_of_age(c->count - used + j));
   // Outputs may not touch the arena (for interleaved entries the sources
   // spread over all of it).
   if (c->slot_numel > 0) {
@@ -114,6 +112,8 @@ int extrapolate_newest(cheb_cache *c, int32_t used, const double *w, int32_t n_o
     if (rc != CHEB_OK) return rc;
     return c->coded->predict(c, 0, used, w, n_out, out, static_cast<hipStream_t>(stream));
   }
+  const void *src[CHEB_MAX_SLOTS];
+  for (int32_t j = 0; j < used; ++j) src[j] = c->slot_ptr(c->slot_of_age(c->count - used + j));
   return combine_checked(src, used, w, n_out, out, c->slot_numel, c->dtype, c->super_vecs,
                          stream);
 }

@@ -1,0 +1,40 @@
+"""The norm calls' host side and the rings under it, without a GPU, built with
+AddressSanitizer and UndefinedBehaviorSanitizer.  clang's also reports
+arithmetic on null pointers."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+ROOT = os.path.dirname(HERE)
+CSRC = os.path.join(ROOT, "paper_2608_23429_amd", "csrc")
+ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
+CLANG = os.path.join(ROCM, "llvm", "bin", "clang++")
+SOURCES = ["api.cpp", "cache.cpp", "table.cpp", "residual.cpp", "coded.cpp", "norm.cpp"]
+
+
+@pytest.mark.parametrize("cxx", [CLANG, "g++"], ids=["clang", "gcc"])
+def test_norm_calls_under_asan_ubsan(tmp_path, cxx):
+    if shutil.which(cxx) is None:
+        pytest.skip("no such compiler")
+    san = ["-fsanitize=address,undefined", "-fno-sanitize-recover=undefined",
+           "-fno-omit-frame-pointer", "-g", "-O1"]
+    inc = ["-I", os.path.join(ROOT, "include"), "-I", CSRC, "-I", os.path.join(ROCM, "include")]
+    objs = []
+    for src in SOURCES + ["host_stubs.cpp", "coded_check.cpp", "norm_check.cpp"]:
+        path = os.path.join(CSRC if src in SOURCES else HERE, src)
+        objs.append(os.path.join(tmp_path, src + ".o"))
+        other_main = ["-Dmain=coded_check_main"] if src == "coded_check.cpp" else []
+        subprocess.run([cxx, "-std=c++17", "-D__HIP_PLATFORM_AMD__", *san, *inc, *other_main,
+                        "-c", path, "-o", objs[-1]], check=True)
+    exe = os.path.join(tmp_path, "norm_check")
+    libdir = os.path.join(ROCM, "lib")
+    subprocess.run([cxx, *san, *objs, "-o", exe, "-L", libdir, "-lamdhip64",
+                    f"-Wl,-rpath,{libdir}", "-lm"], check=True)
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=1",
+               UBSAN_OPTIONS="print_stacktrace=1:halt_on_error=1")
+    r = subprocess.run([exe], capture_output=True, text=True, env=env, timeout=300)
+    assert r.returncode == 0, r.stdout + r.stderr
+    assert "norm ok" in r.stdout
