@@ -500,8 +500,8 @@ class ChebCache:
         return self._h
 
     def _check_here(self, stream: Optional[torch.cuda.Stream], *tensors: torch.Tensor):
-        """Work on 8-bit entries goes to the current device: the cache, the
-        stream and the tensors are all on it."""
+        """Work on 8-bit entries, and reads of any, go to the current device: the
+        cache, the stream and the tensors are all on it."""
         current = torch.cuda.current_device()
         if self.device.index != current or (stream is not None
                                             and stream.device.index != current):
@@ -558,8 +558,7 @@ class ChebCache:
         own, whatever the layout; of 8-bit entries the values of the codes."""
         out = self._new_output(stream) if out is None else out
         self._check_out(out)
-        if self.quant is not None:
-            self._check_here(stream, out)
+        self._check_here(stream, out)
         cheb_cache_read(self._h, idx, out.data_ptr(), _stream_handle(stream))
         return out
 
