@@ -426,6 +426,10 @@ _QUANTS = {None: CHEB_QUANT_NONE, "mxint8": CHEB_QUANT_MXINT8, "mxfp8": CHEB_QUA
 _LAYOUTS = {"slots": CHEB_LAYOUT_SLOTS, "interleaved": CHEB_LAYOUT_INTERLEAVED}
 
 
+class _NoPlace(ChebError, AttributeError):
+    """Where a plain entry lies, asked of 8-bit entries."""
+
+
 class ChebCache:
     """The history ring of one feature set, over a torch-allocated arena.
 
@@ -494,6 +498,13 @@ class ChebCache:
             self.close()
         except Exception:
             pass
+
+    def __getattr__(self, name):
+        if (name in ("slot_stride_bytes", "chunk_elems", "entry_stride_elems")
+                and self.__dict__.get("quant") is not None):
+            raise _NoPlace(_binding.CHEB_E_INVAL, f"{name}: 8-bit entries lie as the library "
+                           "chooses, read() gives them")
+        raise AttributeError(f"{type(self).__name__!r} object has no attribute {name!r}")
 
     @property
     def handle(self):
