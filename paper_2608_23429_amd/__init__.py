@@ -297,6 +297,7 @@ def _norm_call(current, device, x_out, x_in, numel, dim, kind, eps, gain, shift,
         out = _made_for(stream, device, lambda: norm_output(rows, dim, form, device))
     if isinstance(out, (tuple, list)) and len(out) == 2:
         y, scale = out
+        _here(y, "out's codes", current)
         _here(scale, "out's scales", current)
         scale_ptr = scale.data_ptr()
         fmt = CHEB_OUT_FP8_ROW if scale.dtype is torch.float32 else CHEB_OUT_MXFP8
@@ -308,7 +309,7 @@ def _norm_call(current, device, x_out, x_in, numel, dim, kind, eps, gain, shift,
         y, fmt = out, _DTYPES.get(getattr(out, "dtype", None))
         if fmt is None:
             raise ChebError(_binding.CHEB_E_DTYPE, "out is of no supported dtype")
-    _here(y, "out", current)
+        _here(y, "out", current)
     if y.numel() != numel:
         raise ChebError(_binding.CHEB_E_MISMATCH, f"out holds {y.numel()} elements, not {numel}")
     return cheb_norm(rows, dim, eps, in_ptr, out_ptr, gain_ptr, shift_ptr,
