@@ -15,11 +15,11 @@ namespace cheb {
 //  - two runs; one where stores prevail, three outputs or more of three entries
 //    or more (6 entries, 3 outputs of 528 M: 969 us, 988 with two runs; 4
 //    entries, 4 outputs: 492, 505);
-//  - every XCD reading its own copy of a line of scales costs 9% more reads, and
-//    keeping the line's tiles together takes the stores out of their order: that
-//    pays for one output of five entries or more (6 entries of 807 M: 980 us,
-//    1009 without; 3 entries, 1 output: 201, 198 without; 6 entries, 3 outputs:
-//    1007, 969).
+//  - every XCD reading its own copy of a line of scales costs 9% more reads (21%
+//    with tiles of one run), and keeping the line's tiles together takes the stores
+//    out of their order: that pays for one output of five entries or more (6
+//    entries of 807 M: 980 us, 1009 without; 3 entries, 1 output: 201, 198 without;
+//    6 entries, 3 outputs: 1007, 969).
 struct CodedShape {
   int runs;
   bool lines;

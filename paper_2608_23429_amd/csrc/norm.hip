@@ -372,9 +372,9 @@ __device__ __forceinline__ void add_rows(double (&sum)[P][4], double unit, const
 // 1152, one bf16 source, layer norm: 27.8 us for 29.6.)  Sources carry the
 // non-temporal hint, and so does x_out, which is read a whole block later; x_in
 // may be in a cache still, and y is read next.  Measured on MI355X:
-//   8192 x 1152, 6 bf16 entries into MXFP8: 33.0 us, 6.0 TB/s (39.6 without the
-//   hints); 16384 x 1152, layer norm of 4 fp32 entries: 74.5 us, 6.3 TB/s (88);
-//   5003 x 1155 in fp16, a scale a row: 11.1 us.
+//   8192 x 1152, 6 bf16 entries into MXFP8: 33.0 us, 6.0 TB/s (39.7 without the
+//   hints; 6 MXINT8 entries 29.6, MXFP8 27.6); 16384 x 1152, layer norm of 4 fp32
+//   entries: 73.9 us, 6.4 TB/s (88); 5003 x 1155 in fp16, a scale a row: 11.3 us.
 template <class Src, int L, int P, int B, int M>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a) {
   constexpr int kThreads = L < 256 ? 256 : L, kWaves = L > 64 ? L / 64 : 1;
