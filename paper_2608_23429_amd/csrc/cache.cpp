@@ -6,6 +6,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <memory>
 #include <new>
 #include <vector>
 
@@ -211,7 +212,7 @@ GatherPlan next_gather(const GatherSeg *segs, int n, int64_t vec, int64_t super_
 extern "C" {
 
 int cheb_cache_arena_bytes(int32_t n_slots, int32_t dtype, const int64_t *seg_numel,
-                           int32_t n_segs, size_t *arena_bytes, size_t *slot_stride_bytes) {
+                           int32_t n_segs, size_t *arena_bytes, size_t *slot_stride_bytes) try {
   if (!arena_bytes) return fail(CHEB_E_INVAL, "arena_bytes is NULL");
   std::vector<int64_t> off;
   int64_t sn = 0;
@@ -221,11 +222,13 @@ int cheb_cache_arena_bytes(int32_t n_slots, int32_t dtype, const int64_t *seg_nu
   *arena_bytes = ab;
   if (slot_stride_bytes) *slot_stride_bytes = st;
   return ok();
+} catch (const std::bad_alloc &) {
+  return fail(CHEB_E_INVAL, "out of host memory");
 }
 
 int cheb_cache_layout(int32_t n_slots, int32_t dtype, const int64_t *seg_numel, int32_t n_segs,
                       int64_t *seg_offset, int64_t *slot_numel, size_t *slot_stride_bytes,
-                      size_t *arena_bytes) {
+                      size_t *arena_bytes) try {
   std::vector<int64_t> off;
   int64_t sn = 0;
   size_t st = 0, ab = 0;
@@ -236,10 +239,12 @@ int cheb_cache_layout(int32_t n_slots, int32_t dtype, const int64_t *seg_numel, 
   if (slot_stride_bytes) *slot_stride_bytes = st;
   if (arena_bytes) *arena_bytes = ab;
   return ok();
+} catch (const std::bad_alloc &) {
+  return fail(CHEB_E_INVAL, "out of host memory");
 }
 
 int cheb_cache_arena_bytes_ex(int32_t n_slots, int32_t dtype, const int64_t *seg_numel,
-                              int32_t n_segs, int32_t layout_kind, size_t *arena_bytes) {
+                              int32_t n_segs, int32_t layout_kind, size_t *arena_bytes) try {
   if (!arena_bytes) return fail(CHEB_E_INVAL, "arena_bytes is NULL");
   if (!valid_layout(layout_kind)) return fail(CHEB_E_INVAL, "unknown layout %d", layout_kind);
   std::vector<int64_t> off;
@@ -249,11 +254,13 @@ int cheb_cache_arena_bytes_ex(int32_t n_slots, int32_t dtype, const int64_t *seg
   if (rc != CHEB_OK) return rc;
   *arena_bytes = layout_kind == CHEB_LAYOUT_SLOTS ? ab : interleaved_bytes(n_slots, sn, dtype);
   return ok();
+} catch (const std::bad_alloc &) {
+  return fail(CHEB_E_INVAL, "out of host memory");
 }
 
 int cheb_cache_create_ex(cheb_cache **out, int32_t n_slots, int32_t dtype,
                          const int64_t *seg_numel, int32_t n_segs, int32_t layout_kind,
-                         void *arena, size_t arena_bytes) {
+                         void *arena, size_t arena_bytes) try {
   if (!out) return fail(CHEB_E_INVAL, "out is NULL");
   *out = nullptr;
   if (!valid_layout(layout_kind)) return fail(CHEB_E_INVAL, "unknown layout %d", layout_kind);
@@ -267,8 +274,7 @@ int cheb_cache_create_ex(cheb_cache **out, int32_t n_slots, int32_t dtype,
   if (!aligned(arena, kSlotAlign)) return fail(CHEB_E_ALIGN, "arena is not 256-byte aligned");
   if (arena_bytes < need)
     return fail(CHEB_E_MISMATCH, "arena holds %zu bytes, the layout needs %zu", arena_bytes, need);
-  cheb_cache *c = new (std::nothrow) cheb_cache();
-  if (!c) return fail(CHEB_E_INVAL, "out of host memory");
+  std::unique_ptr<cheb_cache> c(new cheb_cache());
   c->n_slots = n_slots;
   c->dtype = dtype;
   c->seg_numel.assign(seg_numel, seg_numel + n_segs);
@@ -283,8 +289,10 @@ int cheb_cache_create_ex(cheb_cache **out, int32_t n_slots, int32_t dtype,
     c->region = reinterpret_cast<char *>((a + kLaneAlign - 1) / kLaneAlign * kLaneAlign);
     c->super_vecs = int64_t(n_slots) * kChunkVecs;
   }
-  *out = c;
+  *out = c.release();
   return ok();
+} catch (const std::bad_alloc &) {
+  return fail(CHEB_E_INVAL, "out of host memory");
 }
 
 int cheb_cache_create(cheb_cache **out, int32_t n_slots, int32_t dtype, const int64_t *seg_numel,
@@ -317,7 +325,7 @@ int cheb_cache_reset(cheb_cache *c) {
   return ok();
 }
 
-int cheb_cache_push(cheb_cache *c, double t, const void *const *seg_src, void *stream) {
+int cheb_cache_push(cheb_cache *c, double t, const void *const *seg_src, void *stream) try {
   if (!c) return fail(CHEB_E_INVAL, "cache is NULL");
   if (c->push_open) return fail(CHEB_E_NOTREADY, "a fused push is open");
   if (!seg_src) return fail(CHEB_E_INVAL, "seg_src is NULL");
@@ -346,6 +354,8 @@ int cheb_cache_push(cheb_cache *c, double t, const void *const *seg_src, void *s
   if (rc != CHEB_OK) return rc;
   record(c, t);
   return ok();
+} catch (const std::bad_alloc &) {
+  return fail(CHEB_E_INVAL, "out of host memory");
 }
 
 int cheb_cache_begin_push(cheb_cache *c, void **slot_base) {

@@ -9,6 +9,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <new>
 #include <vector>
 
 #include "cache.h"
@@ -100,6 +101,7 @@ int run(const std::vector<Interval> &plan_iv, int vec, DeltaFn delta_of, const f
     }
     return launch(delta.data(), int(covers), parts, n_parts, x_in);
   }
+  delta.reserve(max_cover);  // nothing can fail between the launches but they
   for (const Interval &iv : plan_iv) {
     size_t first = 0;
     do {
@@ -131,7 +133,7 @@ int launch_plain(int dtype, int n, const uint64_t *base, const double *w, const 
 extern "C" {
 
 int cheb_residual_apply(cheb_cache *c, const double *w, const int64_t *res_offset,
-                        int64_t res_numel, const float *x_in, float *x_out, void *stream) {
+                        int64_t res_numel, const float *x_in, float *x_out, void *stream) try {
   CacheView v;
   int rc = cache_view(c, &v);
   if (rc != CHEB_OK) return rc;
@@ -173,11 +175,13 @@ int cheb_residual_apply(cheb_cache *c, const double *w, const int64_t *res_offse
                return launch_plain(v.dtype, v.n_slots, base, w, delta, n_delta, parts, n_parts, in,
                                    x_out, v.super_vecs, s);
              });
+} catch (const std::bad_alloc &) {
+  return fail(CHEB_E_INVAL, "out of host memory");
 }
 
 int cheb_residual_reduce(const void *const *seg_src, const int64_t *seg_numel,
                          const int64_t *res_offset, int32_t n_segs, int32_t dtype,
-                         const float *x_in, float *x_out, int64_t res_numel, void *stream) {
+                         const float *x_in, float *x_out, int64_t res_numel, void *stream) try {
   if (!valid_dtype(dtype)) return fail(CHEB_E_DTYPE, "unknown dtype %d", dtype);
   if (!seg_src || !seg_numel || !res_offset) return fail(CHEB_E_INVAL, "segment arrays NULL");
   if (n_segs < 1) return fail(CHEB_E_INVAL, "n_segs must be at least 1");
@@ -205,6 +209,8 @@ int cheb_residual_reduce(const void *const *seg_src, const int64_t *seg_numel,
                return launch_plain(dtype, 1, base, one, delta, n_delta, parts, n_parts, in, x_out,
                                    kChunkVecs, static_cast<hipStream_t>(stream));
              });
+} catch (const std::bad_alloc &) {
+  return fail(CHEB_E_INVAL, "out of host memory");
 }
 
 }  // extern "C"

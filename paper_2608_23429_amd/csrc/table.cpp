@@ -10,6 +10,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <memory>
 #include <new>
 #include <vector>
 
@@ -90,7 +91,7 @@ int cheb_schedule(int32_t T, int32_t s0, int32_t s1, int32_t r, uint8_t *is_full
 }
 
 int cheb_table_build(cheb_table **out, int32_t T, int32_t s0, int32_t s1, int32_t r,
-                     int32_t n_hist, const double *abscissa, int32_t policy) {
+                     int32_t n_hist, const double *abscissa, int32_t policy) try {
   if (!out) return fail(CHEB_E_INVAL, "out is NULL");
   *out = nullptr;
   if (!schedule_args_ok(T, s0, s1, r))
@@ -102,8 +103,7 @@ int cheb_table_build(cheb_table **out, int32_t T, int32_t s0, int32_t s1, int32_
   if (!abscissa) return fail(CHEB_E_INVAL, "abscissa is NULL");
   for (int32_t s = 0; s < T; ++s)
     if (!isfinite(abscissa[s])) return fail(CHEB_E_NONFINITE, "abscissa of step %d", s);
-  cheb_table *t = new (std::nothrow) cheb_table();
-  if (!t) return fail(CHEB_E_INVAL, "out of host memory");
+  std::unique_ptr<cheb_table> t(new cheb_table());
   t->T = T;
   t->s0 = s0;
   t->s1 = s1;
@@ -113,17 +113,16 @@ int cheb_table_build(cheb_table **out, int32_t T, int32_t s0, int32_t s1, int32_
   t->abscissa.assign(abscissa, abscissa + T);
   std::vector<uint8_t> scheduled(static_cast<size_t>(T), 0);
   for (int32_t s = 0; s < T; ++s) scheduled[size_t(s)] = in_schedule(T, s0, s1, r, s) ? 1 : 0;
-  int rc = fill_rows(t, scheduled.data());
-  if (rc != CHEB_OK) {
-    delete t;
-    return rc;
-  }
-  *out = t;
+  int rc = fill_rows(t.get(), scheduled.data());
+  if (rc != CHEB_OK) return rc;
+  *out = t.release();
   return ok();
+} catch (const std::bad_alloc &) {
+  return fail(CHEB_E_INVAL, "out of host memory");
 }
 
 int cheb_table_build_mask(cheb_table **out, int32_t T, const uint8_t *is_full, int32_t n_hist,
-                          const double *abscissa, int32_t policy) {
+                          const double *abscissa, int32_t policy) try {
   if (!out) return fail(CHEB_E_INVAL, "out is NULL");
   *out = nullptr;
   if (T < 1 || T > kMaxSteps) return fail(CHEB_E_INVAL, "T %d outside 1..%d", T, kMaxSteps);
@@ -134,8 +133,7 @@ int cheb_table_build_mask(cheb_table **out, int32_t T, const uint8_t *is_full, i
     return fail(CHEB_E_INVAL, "unknown short-history policy %d", policy);
   for (int32_t s = 0; s < T; ++s)
     if (!isfinite(abscissa[s])) return fail(CHEB_E_NONFINITE, "abscissa of step %d", s);
-  cheb_table *t = new (std::nothrow) cheb_table();
-  if (!t) return fail(CHEB_E_INVAL, "out of host memory");
+  std::unique_ptr<cheb_table> t(new cheb_table());
   // A mask table records no (s0, s1, r); saved tables carry r = 0 to say so.
   t->T = T;
   t->s0 = 0;
@@ -146,13 +144,12 @@ int cheb_table_build_mask(cheb_table **out, int32_t T, const uint8_t *is_full, i
   t->abscissa.assign(abscissa, abscissa + T);
   std::vector<uint8_t> scheduled(is_full, is_full + T);
   for (uint8_t &v : scheduled) v = v ? 1 : 0;
-  int rc = fill_rows(t, scheduled.data());
-  if (rc != CHEB_OK) {
-    delete t;
-    return rc;
-  }
-  *out = t;
+  int rc = fill_rows(t.get(), scheduled.data());
+  if (rc != CHEB_OK) return rc;
+  *out = t.release();
   return ok();
+} catch (const std::bad_alloc &) {
+  return fail(CHEB_E_INVAL, "out of host memory");
 }
 
 int cheb_table_destroy(cheb_table *t) {
@@ -237,11 +234,16 @@ int cheb_table_load(cheb_table **out, const char *path) {
       tmp.n_hist > CHEB_MAX_SLOTS || (tmp.policy != 0 && tmp.policy != 1))
     return bad("parameters out of range");
   const int32_t T = tmp.T, n = tmp.n_hist;
-  tmp.abscissa.assign(size_t(T), 0.0);
-  tmp.predicted.assign(size_t(T), 0);
-  tmp.n_used.assign(size_t(T), 0);
-  tmp.nodes.assign(size_t(T) * n, -1);
-  tmp.w.assign(size_t(T) * n, 0.0);
+  try {
+    tmp.abscissa.assign(size_t(T), 0.0);
+    tmp.predicted.assign(size_t(T), 0);
+    tmp.n_used.assign(size_t(T), 0);
+    tmp.nodes.assign(size_t(T) * n, -1);
+    tmp.w.assign(size_t(T) * n, 0.0);
+  } catch (const std::bad_alloc &) {
+    fclose(f);
+    return fail(CHEB_E_INVAL, "out of host memory");
+  }
   char kind[16];
   for (int32_t s = 0; s < T; ++s) {
     int idx = -1;
