@@ -311,10 +311,9 @@ CHEB_API int cheb_cache_reset(cheb_cache *c);
  *                      beside a large one.
  * A group with a NaN or an infinity reads back as NaN, all of it.  A value
  * whose code stands for more than the storage type holds reads back as infinity
- * (fp16: beyond 65023 for MXINT8, 63487 for MXFP8); residual updates and norms
- * take it for what the code stands for.  Predictions sum in fp32 for
- * bf16 and fp16 caches and in fp64 for fp32 ones; residual updates sum in fp64
- * for all of them. */
+ * (fp16: beyond 65023 for MXINT8, 63487 for MXFP8); other calls take it for what
+ * the code stands for.  Predictions sum in fp32 for bf16 and fp16 caches and in
+ * fp64 for fp32 ones; residual updates and norms sum in fp64 for all of them. */
 enum { CHEB_QUANT_NONE = 0, CHEB_QUANT_MXINT8 = 1, CHEB_QUANT_MXFP8 = 2 };
 
 /* The layout of a history of 8-bit entries: as cheb_cache_layout, but cached
